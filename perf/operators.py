@@ -201,7 +201,7 @@ def _captured(case, s):
         y = out["y"] = node("attention", [q, k, v] + lengths, s["q"].shape, **how)
         if case["backward"]:
             dy = given("dy")
-            rows = node("attention_rows", [dy, y], (case["n"], 2 * case["heads"], 1, case["Tq"]), heads=case["heads"])
+            rows = node("attention_rows", [dy, y], (case["n"], 3 * case["heads"], 1, case["Tq"]), heads=case["heads"])
             for name, of in (("dq", "q"), ("dk", "k"), ("dv", "v")):
                 out[name] = node("attention_" + name, [dy, rows, q, k, v] + lengths, s[of].shape, **how)
     if not _origin:
