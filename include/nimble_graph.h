@@ -85,9 +85,32 @@ enum {
     NG_OP_SLICE_PAD = 23,     /* preds {dy}: gradient of one concat input. Result has cout channels; its channels
                                  [slice_lo[1], slice_lo[1] + cnt) are dy's channels [slice_lo[0], slice_hi[0]),
                                  cnt = slice_hi[0] - slice_lo[0]; every other channel is 0 */
-    NG_OP_SGD_UPDATE = 24     /* preds {grad, then any nodes that must have run first (readers of W)}, weights {W}:
+    NG_OP_SGD_UPDATE = 24,    /* preds {grad, then any nodes that must have run first (readers of W)}, weights {W}:
                                  W[i] -= lr * grad[slice_lo[0] + i] for i < cout, IN PLACE in the caller's buffer;
                                  the node's own result is [1][1][1][1] */
+    /* Attention. A sequence is an image whose h x w pixels are its tokens (T = h w), a head a run of d consecutive channels,
+     * c = heads d: what a 1 x 1 convolution leaves and takes. */
+    NG_OP_HEAD_ROPE = 25,     /* preds {x, positions}, weights {frequencies[rot / 2]} or {frequencies[rot / 2], gamma[d]}: the norm of
+                                 each head (with gamma) and its rotation by the token's position. d = c / heads <= 256;
+                                   u[c] = x[c] gamma[c] / sqrt(mean over the head of x^2 + eps)       (without gamma: u = x)
+                                   (a, b) -> factor (a cos t - b sin t, a sin t + b cos t), t = position * frequencies[i], for the
+                                 pairs i < rot / 2 of the head's first rot channels (rot even, 2 .. d): channels (2 i, 2 i + 1) if
+                                 interleaved != 0, else (i, i + rot / 2); the channels from rot on are u. positions: [1][1] or
+                                 [n][1] x tokens of x, any finite numbers; no gradient goes to them */
+    NG_OP_HEAD_ROPE_DGRAD = 26, /* preds {dy, x, positions}, same weights and parameters -> dx */
+    NG_OP_HEAD_ROPE_WGRAD = 27, /* preds {dy, x, positions}, weights {frequencies, gamma} -> dgamma as [1][d][1][1] */
+    NG_OP_ATTENTION = 28,     /* preds {q, k, v} or {q, k, v, lengths}, no weights. q has c = heads d channels and Tq tokens, k and v
+                                 have kv_heads d channels and Tk tokens, of another sequence or of the same one; d <= 128; query
+                                 head i reads key head i / (heads / kv_heads), kv_heads a divisor of heads. lengths [n][1][1][1]:
+                                 image b has the keys j < lengths[b] (not a number: none), whatever lies behind them in k and v;
+                                 y[i] = sum_j p[i][j] v[j], p[i][.] = softmax over these keys of scale <q[i], k[j]>; a query
+                                 without any key: 0. q, and the keys and values that count, have to be finite */
+    NG_OP_ATTENTION_ROWS = 29, /* preds {dy, y}, y an NG_OP_ATTENTION node, heads as there -> [n][3 heads] x tokens of y: for each query
+                                 <dy, y> of its head, the largest score (times log2 e) of its keys, and one over the sum of their
+                                 2^(score - largest); 0 and 0 without any key. What the three gradients need of every query */
+    NG_OP_ATTENTION_DQ = 30,  /* preds {dy, rows, q, k, v[, lengths]} of one attention, heads, kv_heads and scale as there; rows: its */
+    NG_OP_ATTENTION_DK = 31,  /* NG_OP_ATTENTION_ROWS node -> dq, dk (shapes of q, k; 0 for keys that do not count) */
+    NG_OP_ATTENTION_DV = 32   /* -> dv */
 };
 
 typedef struct ng_op_params {
@@ -97,10 +120,16 @@ typedef struct ng_op_params {
     int32_t pad;       /* CONV3X3, POOL: 0 or 1 */
     int32_t relu;      /* BN_ACT */
     int32_t pool_mode; /* POOL: 0 max, 1 avg */
-    float eps;         /* BN_ACT */
+    float eps;         /* BN_ACT, HEAD_ROPE* */
     int32_t slice_lo[NG_MAX_PREDS]; /* CONCAT; slice_hi[j] == 0 means "all channels of pred j" */
     int32_t slice_hi[NG_MAX_PREDS];
     float lr;          /* SGD_UPDATE */
+    int32_t heads;     /* HEAD_ROPE*, ATTENTION*: heads of x, of q */
+    int32_t kv_heads;  /* ATTENTION, _DQ, _DK, _DV: heads of k and v */
+    int32_t rot;       /* HEAD_ROPE*: channels of a head that are rotated */
+    int32_t interleaved; /* HEAD_ROPE*: which channels are a pair */
+    float factor;      /* HEAD_ROPE*: on the rotated channels (1: a rotation; scaled long contexts may want another) */
+    float scale;       /* ATTENTION, _DQ, _DK, _DV: on the scores */
 } ng_op_params;
 
 typedef struct ng_graph ng_graph; /* opaque */

@@ -29,7 +29,8 @@ from typing import Dict, List, Optional, Tuple
 
 import numpy as np
 
-from .forward import eval_node
+from . import ops
+from .forward import eval_node, input_value
 
 
 def _f64(x):
@@ -113,6 +114,45 @@ def pool3x3_vjp(x, mode, stride, pad, dy):
     return _unpad(dxp, pad)
 
 
+def head_rope_vjp(x, positions, freq, gamma, heads, interleaved, eps, factor, dy):
+    """The rotation's transpose takes dy back to du; through u = gamma x / rms: dx = (gamma du - xh mean(gamma du xh)) / rms with
+    xh = x / rms, dgamma = sum du xh. (dx, dgamma or None); no gradient goes to the positions."""
+    x, dy = _f64(x), _f64(dy)
+    n, c, h, w = x.shape
+    shape = (n, heads, c // heads, h * w)
+    x, g = x.reshape(shape), dy.reshape(shape)
+    t = ops.rope_angles(positions, freq, n)[:, None]
+    ia, ib = ops.rope_pair_channels(2 * len(freq), interleaved)
+    du = g.copy()
+    du[:, :, ia] = factor * (g[:, :, ia] * np.cos(t) + g[:, :, ib] * np.sin(t))
+    du[:, :, ib] = factor * (g[:, :, ib] * np.cos(t) - g[:, :, ia] * np.sin(t))
+    if gamma is None:
+        return du.reshape(n, c, h, w), None
+    rms = np.sqrt((x * x).mean(axis=2, keepdims=True) + eps)
+    xh = x / rms
+    gu = du * _f64(gamma)[None, None, :, None]
+    dx = (gu - xh * (gu * xh).mean(axis=2, keepdims=True)) / rms
+    return dx.reshape(n, c, h, w), (du * xh).sum(axis=(0, 1, 3))
+
+
+def attention_vjp(q, k, v, lengths, heads, kv_heads, scale, dy):
+    """dv = p^T dy; ds = p (dp - <p, dp>) with dp = <dy, v>; dq = scale ds k, dk = scale ds^T q; heads that share a key head add up."""
+    p = ops.attention_weights(q, k, heads, kv_heads, scale, lengths)
+    n, group = p.shape[0], heads // kv_heads
+    qh, gh = (_f64(t).reshape(n, heads, -1, p.shape[2]) for t in (q, dy))
+    kh, vh = (ops.counted_values(t, kv_heads, lengths) for t in (k, v))
+    dq, dk, dv = np.zeros_like(qh), np.zeros_like(kh), np.zeros_like(vh)
+    for b in range(n):
+        for h in range(heads):
+            j = h // group
+            dv[b, j] += gh[b, h] @ p[b, h]
+            dp = gh[b, h].T @ vh[b, j]
+            ds = p[b, h] * (dp - (p[b, h] * dp).sum(axis=1, keepdims=True))
+            dq[b, h] = scale * (kh[b, j] @ ds.T)
+            dk[b, j] += scale * (qh[b, h] @ ds)
+    return dq.reshape(np.shape(q)), dk.reshape(np.shape(k)), dv.reshape(np.shape(v))
+
+
 def node_vjp(nd, ins, dy) -> Tuple[List[np.ndarray], List[np.ndarray]]:
     """(gradients w.r.t. the node's inputs, gradients w.r.t. its weight tensors)."""
     p, w = nd.params, nd.weights
@@ -148,6 +188,13 @@ def node_vjp(nd, ins, dy) -> Tuple[List[np.ndarray], List[np.ndarray]]:
     if nd.op == "fc":
         x, dyf = _f64(ins[0]).reshape(ins[0].shape[0], -1), _f64(dy).reshape(dy.shape[0], -1)
         return [(dyf @ _f64(w[0])).reshape(ins[0].shape)], [dyf.T @ x, dyf.sum(axis=0)]
+    if nd.op == "head_rope":
+        dx, dg = head_rope_vjp(ins[0], ins[1], w[0], w[1] if len(w) > 1 else None, p["heads"], bool(p["interleaved"]), p["eps"], p["factor"], dy)
+        return [dx, np.zeros(ins[1].shape)], [np.zeros(len(w[0]))] + ([dg] if dg is not None else [])
+    if nd.op == "attention":
+        lengths = ins[3] if len(ins) > 3 else None
+        grads = attention_vjp(ins[0], ins[1], ins[2], lengths, p["heads"], p["kv_heads"], p["scale"], dy)
+        return list(grads) + ([np.zeros(lengths.shape)] if lengths is not None else []), []
     raise ValueError(f"unknown op {nd.op!r}")
 
 
@@ -158,7 +205,7 @@ def backward(workload, seed: Dict[int, np.ndarray], x: Optional[np.ndarray] = No
     x = workload.input if x is None else x
     val: Dict[int, np.ndarray] = {}
     for v, nd in enumerate(nodes):
-        val[v] = np.asarray(x) if nd.op == "input" else eval_node(nd, [val[u] for u in nd.preds])
+        val[v] = np.asarray(input_value(workload, v, x)) if nd.op == "input" else eval_node(nd, [val[u] for u in nd.preds])
     d_value = {v: np.zeros(val[v].shape) for v in range(len(nodes))}
     d_weight: Dict[int, List[np.ndarray]] = {}
     for o, s in seed.items():

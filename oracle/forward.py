@@ -35,7 +35,16 @@ def eval_node(nd, ins):
         return ops.global_avgpool(ins[0])
     if nd.op == "fc":
         return ops.fc(ins[0], w[0], w[1])
+    if nd.op == "head_rope":
+        return ops.head_rope(ins[0], ins[1], w[0], w[1] if len(w) > 1 else None, p["heads"], bool(p["interleaved"]), p["eps"], p["factor"])
+    if nd.op == "attention":
+        return ops.attention(ins[0], ins[1], ins[2], ins[3] if len(ins) > 3 else None, p["heads"], p["kv_heads"], p["scale"])
     raise ValueError(f"unknown op {nd.op!r}")
+
+
+def input_value(workload, v, x):
+    """The value of input node v: x for node 0, the workload's own for further ones."""
+    return x if v == 0 else workload.inputs[v]
 
 
 def forward(workload, x: Optional[np.ndarray] = None, keep: Optional[Iterable[int]] = None) -> Dict[int, np.ndarray]:
@@ -52,8 +61,9 @@ def forward(workload, x: Optional[np.ndarray] = None, keep: Optional[Iterable[in
     out: Dict[int, np.ndarray] = {}
     for v, nd in enumerate(nodes):
         if nd.op == "input":
-            assert tuple(x.shape) == (nd.params["n"], nd.params["c"], nd.params["h"], nd.params["w"])
-            val[v] = np.ascontiguousarray(x, dtype=np.float32)
+            t = input_value(workload, v, x)
+            assert tuple(t.shape) == (nd.params["n"], nd.params["c"], nd.params["h"], nd.params["w"])
+            val[v] = np.ascontiguousarray(t, dtype=np.float32)
         else:
             val[v] = eval_node(nd, [val[u] for u in nd.preds])
         if v in keep:

@@ -129,3 +129,68 @@ def fc(x, w, b):
     n, c, h, wd = x.shape
     assert h == 1 and wd == 1
     return _out((x.reshape(n, c) @ w.T + b[None]).reshape(n, -1, 1, 1))
+
+
+def rope_angles(positions, freq, n):
+    """[n, rot / 2, tokens]: angle of every pair at every token."""
+    pos = _f64(positions).reshape(np.shape(positions)[0], 1, -1)
+    return np.broadcast_to(pos * _f64(freq)[None, :, None], (n, len(freq), pos.shape[2]))
+
+
+def rope_pair_channels(rot: int, interleaved: bool):
+    """First and second channels of the rotated pairs of a head."""
+    i = np.arange(rot // 2)
+    return (2 * i, 2 * i + 1) if interleaved else (i, i + rot // 2)
+
+
+def head_rope(x, positions, freq, gamma, heads: int, interleaved: bool, eps: float, factor: float):
+    """Each head (a run of channels): x gamma / sqrt(mean x^2 + eps) (gamma None: x), then its first 2 len(freq) channels rotated in
+    pairs by position * freq and multiplied by factor."""
+    x = _f64(x)
+    n, c, h, w = x.shape
+    u = x.reshape(n, heads, c // heads, h * w)
+    if gamma is not None:
+        u = u / np.sqrt((u * u).mean(axis=2, keepdims=True) + eps) * _f64(gamma)[None, None, :, None]
+    y = u.copy()
+    t = rope_angles(positions, freq, n)[:, None]
+    ia, ib = rope_pair_channels(2 * len(freq), interleaved)
+    y[:, :, ia] = factor * (u[:, :, ia] * np.cos(t) - u[:, :, ib] * np.sin(t))
+    y[:, :, ib] = factor * (u[:, :, ia] * np.sin(t) + u[:, :, ib] * np.cos(t))
+    return _out(y.reshape(n, c, h, w))
+
+
+def key_count(length, tk: int) -> int:
+    """Keys j < length; none if it is not a number."""
+    return sum(1 for j in range(tk) if j < length)
+
+
+def attention_weights(q, k, heads: int, kv_heads: int, scale: float, lengths):
+    """p[n][head][query][key]: softmax over the keys that count, 0 for the others (and everywhere for an image without any)."""
+    q, k = _f64(q), _f64(k)
+    n, c = q.shape[:2]
+    q, k = q.reshape(n, heads, c // heads, -1), k.reshape(n, kv_heads, c // heads, -1)
+    p = np.zeros((n, heads, q.shape[3], k.shape[3]))
+    for b in range(n):
+        m = k.shape[3] if lengths is None else key_count(float(np.ravel(lengths)[b]), k.shape[3])
+        for h in range(heads if m else 0):
+            s = scale * (q[b, h].T @ k[b, h // (heads // kv_heads)][:, :m])
+            e = np.exp(s - s.max(axis=1, keepdims=True))
+            p[b, h, :, :m] = e / e.sum(axis=1, keepdims=True)
+    return p
+
+
+def counted_values(v, kv_heads: int, lengths):
+    """v by heads, zeros in the place of what does not count."""
+    v = _f64(v)
+    v = v.reshape(v.shape[0], kv_heads, v.shape[1] // kv_heads, -1).copy()
+    for b in range(v.shape[0] if lengths is not None else 0):
+        v[b, :, :, key_count(float(np.ravel(lengths)[b]), v.shape[3]):] = 0.0
+    return v
+
+
+def attention(q, k, v, lengths, heads: int, kv_heads: int, scale: float):
+    """y[query] = sum over keys p[query][key] v[key]."""
+    p = attention_weights(q, k, heads, kv_heads, scale, lengths)
+    vh = counted_values(v, kv_heads, lengths)
+    y = np.stack([np.stack([vh[b, h // (heads // kv_heads)] @ p[b, h].T for h in range(heads)]) for b in range(p.shape[0])])
+    return _out(y.reshape(q.shape))

@@ -49,8 +49,14 @@ enum Kid : int {
     // two tasks that read the same gradient, in one launch (likewise): depthwise input and weight gradient, dealt out alternately;
     // conv1x1 input gradient with the weight gradient in blocks of 16 x 16 / 32 x 32 (pw_backward_share)
     KID_PAIR_DW, KID_PAIR_DW_LDS, KID_PAIR_PW16, KID_PAIR_PW32,
+    // attention: norm and rotation of heads (4 / 8: up to 128 / 256 channels a head; N: few tokens an image), and their gradients
+    KID_ROPE_4, KID_ROPE_8, KID_ROPE_N, KID_ROPE_DX_4, KID_ROPE_DX_8, KID_ROPE_DX_N, KID_ROPE_DG_4, KID_ROPE_DG_8, KID_ROPE_DG_N,
+    KID_ATTN_ROWS,
+    // a wavefront owns 16 queries (DK, DV: 16 keys) of heads of up to 64 / 128 channels and reads its operands straight from memory
+    KID_ATTN_W64, KID_ATTN_W128, KID_ATTN_DQ_W64, KID_ATTN_DQ_W128, KID_ATTN_DK_W64, KID_ATTN_DK_W128, KID_ATTN_DV_W64, KID_ATTN_DV_W128,
     KID_COUNT
 };
+constexpr bool is_attention_kernel(int kid) { return kid >= KID_ROPE_4 && kid < KID_COUNT; }
 constexpr bool is_train_kernel(int kid) { return kid >= KID_GEMM_PW_FWD && kid <= KID_SGD; }
 
 // the variant without / with a fused add_n of a kernel (ids without such a variant map to themselves / KID_NONE)
@@ -116,14 +122,16 @@ constexpr bool is_matrix_kernel(int kid_any) {
 // conv1x1 and the vector-ALU conv3x3 (kernels of large problems with large register needs)
 constexpr bool is_lean_kernel(int kid) {
     return (!(kid >= KID_PW_D4 && kid <= KID_C3_T8S2) || kid == KID_C3_T16S2 || kid == KID_C3_T8S2) && kid != KID_C3_L32 && kid != KID_C3_L64 && !is_c3_patch(kid) && !is_pw_patch(kid) && !is_large_tensor_kernel(kid) &&
-           !is_train_kernel(kid) && !(kid >= KID_SGD_BATCH && kid <= KID_PAIR_PW32);
+           !is_train_kernel(kid) && !(kid >= KID_SGD_BATCH && kid <= KID_PAIR_PW32) && !is_attention_kernel(kid);
 }
-// Three builds of the resident kernel: lean (small inference problems), full (every inference kernel), train (the lean
+// Four builds of the resident kernel: lean (small inference problems), full (every inference kernel), train (the lean
 // kernels plus the training kernels: a graph that trains runs its convolutions through the GEMM kernels, never through
-// the repacked-weight kernels of the full build).
-enum { BUILD_LEAN = 0, BUILD_FULL = 1, BUILD_TRAIN = 2 };
+// the repacked-weight kernels of the full build), attention (the lean kernels plus the attention kernels: the other three keep the
+// registers that they had without those. All kernels in one build take 330 s to compile instead of 120, for graphs whose tasks are
+// too large to gain from this mode).
+enum { BUILD_LEAN = 0, BUILD_FULL = 1, BUILD_TRAIN = 2, BUILD_ATTENTION = 3 };
 constexpr bool in_build(int build, int kid) {
-    return (kid >= KID_SGD_BATCH && kid <= KID_PAIR_PW32) ? false : build == BUILD_LEAN ? is_lean_kernel(kid) : build == BUILD_FULL ? !is_train_kernel(kid) : (is_lean_kernel(kid) || is_train_kernel(kid) || is_large_tensor_kernel(kid));
+    return (kid >= KID_SGD_BATCH && kid <= KID_PAIR_PW32) ? false : build == BUILD_ATTENTION ? is_lean_kernel(kid) || is_attention_kernel(kid) : is_attention_kernel(kid) ? false : build == BUILD_LEAN ? is_lean_kernel(kid) : build == BUILD_FULL ? !is_train_kernel(kid) : (is_lean_kernel(kid) || is_train_kernel(kid) || is_large_tensor_kernel(kid));
 }
 
 constexpr int kBlock = 256;          // threads that work on one tile (a stand-alone kernel's workgroup)
@@ -379,6 +387,41 @@ struct SgdTile {
 };
 struct SgdBatchArgs {
     const SgdTile* tiles;      // [ntiles]
+};
+
+// ---- attention ---------------------------------------------------------------------------
+constexpr int kRopeMaxHead = 256, kAttentionMaxHead = 128;   // channels of a head
+struct RopeArgs {
+    const float* x;            // [n][heads d][T]
+    const float* dy;           // gradients: of the result
+    const float* pos;          // [T] or [n][T]
+    const float* freq;         // [rot / 2]
+    const float* gamma;        // [d], nullptr: no norm
+    float* y;                  // forward: y; dgrad: dx
+    float* ws;                 // wgrad: sums of each workgroup [tiles][d]
+    unsigned* cnt;             // wgrad: arrivals, zero between replays
+    float* dg;                 // wgrad: dgamma [d]
+    float eps, factor;
+    int N, H, d, T, rot, interleaved;
+    int pos_stride;            // T, or 0 if all images have the same positions
+    int blocks;                // blocks of 64 tokens of an image (few tokens an image: 0)
+    int heads_per_tile;        // heads that a workgroup walks with the angles of one block
+    int items, per_tile;       // blocks of all images (few tokens: tokens x heads of all images in groups of four wavefronts), and how many of them a workgroup walks
+    int tiles;
+};
+struct AttnArgs {
+    const float* q; const float* k; const float* v;
+    const float* len;          // [n] or nullptr: every image has Tk keys
+    const float* dy;           // gradients
+    const float* rows;         // gradients: [n][3][H][Tq]
+    float* y;                  // the result: y, dq, dk or dv
+    float* stats;              // forward: [2][n][H][Tq] largest score, one over the sum (nullptr: nobody reads them); rows: read
+    float* ws;                 // splits > 1: partial results of each split
+    unsigned* cnt;             // splits > 1: arrivals for each block of the result, zero between replays
+    float scale, scale_log2;   // scale_log2 = scale log2 e
+    int N, H, Hk, d, Tq, Tk;
+    int col_blocks;            // blocks of columns (queries of the heads that share a key head; dk, dv: keys) for each image and key head
+    int splits, per_split;     // the other side (keys; dk, dv: queries) is cut into splits of per_split blocks
 };
 
 // Two tasks in one launch: tiles of both, dealt out alternately while both have tiles left (depthwise; conv1x1: pw_backward_share).

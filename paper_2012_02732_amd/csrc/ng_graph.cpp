@@ -2,6 +2,7 @@
 // Paper: Nimble (arXiv 2012.02732), Section 4 (input is a static operator DAG with a
 // fixed input shape) and Section 4.1 (all shapes and all memory are fixed ahead of time).
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <new>
@@ -17,6 +18,10 @@ int conv_out(int64_t size, int k, int stride, int pad) {
 }
 
 bool in_set(int v, int a, int b) { return v == a || v == b; }
+
+// Attention operators address one head of one image (attention: the heads of q that share a key head) by 32-bit byte offsets.
+constexpr int64_t kMaxSliceElems = (int64_t)1 << 29;
+constexpr int64_t kMaxAttentionTiles = (int64_t)1 << 22;     // blocks of 16 columns; a launch has fewer than 2^24 workgroups
 
 // Output shape of an operator, or an error text. Mirrors the operator table in the header.
 const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* preds, int n_preds,
@@ -211,6 +216,76 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
             if (!(p.lr == p.lr)) return "sgd_update: lr is not a number";
             out = Shape{1, 1, 1, 1};
             return nullptr;
+        case NG_OP_HEAD_ROPE:
+        case NG_OP_HEAD_ROPE_DGRAD:
+        case NG_OP_HEAD_ROPE_WGRAD: {
+            const bool backward = op != NG_OP_HEAD_ROPE, wgrad = op == NG_OP_HEAD_ROPE_WGRAD;
+            if (n_preds != (backward ? 3 : 2) || (n_weights != 2 && (wgrad || n_weights != 1)))
+                return backward ? "head_rope backward takes dy, x and positions, and the frequencies and gamma of the forward operator (dgrad: gamma if it has one)"
+                                : "head_rope takes x and positions, and 1 or 2 weights (frequencies, gamma)";
+            const Shape &x = in(backward ? 1 : 0), &pos = in(backward ? 2 : 1);
+            if (p.heads <= 0 || x.c % p.heads != 0) return "head_rope: heads must divide the channels of x";
+            const int64_t d = x.c / p.heads;
+            if (d > kRopeMaxHead) return "head_rope: a head has at most 256 channels";
+            if (p.rot < 2 || p.rot % 2 != 0 || p.rot > d) return "head_rope: rot must be even, 2 .. channels of a head";
+            if (!in_set(p.interleaved, 0, 1)) return "head_rope: interleaved in {0,1}";
+            if (!(p.eps >= 0.f) || !std::isfinite(p.eps)) return "head_rope: eps must be >= 0 and finite";
+            if (!std::isfinite(p.factor)) return "head_rope: factor must be finite";
+            code = NG_ESHAPE;
+            if (backward && !(in(0) == x)) return "head_rope backward: dy and x differ in shape";
+            if ((pos.n != 1 && pos.n != x.n) || pos.c != 1 || pos.h != x.h || pos.w != x.w)
+                return "head_rope: positions must be [1 or n][1][h][w] for x [n][c][h][w]";
+            if (d * x.h * x.w > kMaxSliceElems) return "head_rope: a head of one image has more than 2^29 values";
+            out = wgrad ? Shape{1, d, 1, 1} : x;
+            return nullptr;
+        }
+        case NG_OP_ATTENTION:
+        case NG_OP_ATTENTION_DQ:
+        case NG_OP_ATTENTION_DK:
+        case NG_OP_ATTENTION_DV: {
+            const int first = op == NG_OP_ATTENTION ? 0 : 2;           // behind dy and rows
+            if ((n_preds != first + 3 && n_preds != first + 4) || n_weights != 0)
+                return first ? "attention backward takes dy, rows, q, k, v and, if the attention has them, lengths" : "attention takes q, k, v and, if wanted, lengths";
+            const Shape &q = in(first), &k = in(first + 1), &v = in(first + 2);
+            if (p.heads <= 0 || p.kv_heads <= 0 || p.heads % p.kv_heads != 0) return "attention: kv_heads must be positive and divide heads";
+            if (!std::isfinite(p.scale)) return "attention: scale must be finite";
+            code = NG_ESHAPE;
+            if (q.c % p.heads != 0 || q.c / p.heads > kAttentionMaxHead) return "attention: heads must divide the channels of q, at most 128 channels a head";
+            const int64_t d = q.c / p.heads;
+            if (!(k == v) || k.n != q.n || k.c != d * p.kv_heads) return "attention: k and v must be [n][kv_heads * channels of a head] x tokens for q [n][heads * channels of a head]";
+            const int64_t Tq = q.h * q.w, Tk = k.h * k.w;
+            if (Tq * d * (p.heads / p.kv_heads) > kMaxSliceElems || Tk * d > kMaxSliceElems)
+                return "attention: a head of k, or the heads of q that read it, have more than 2^29 values";
+            if (q.n * p.kv_heads * ((std::max(Tq * (p.heads / p.kv_heads), Tk) + 15) / 16) > kMaxAttentionTiles) return "attention: too many heads and tokens for one launch";
+            if (n_preds == first + 4 && !(in(first + 3) == Shape{q.n, 1, 1, 1})) return "attention: lengths must be [n][1][1][1]";
+            if (first) {
+                if (!(in(0) == q)) return "attention backward: dy and q differ in shape";
+                const Node& rows = g->nodes[preds[1]];
+                code = NG_EINVAL;
+                if (rows.op != NG_OP_ATTENTION_ROWS || rows.preds[0] != preds[0]) return "attention backward: the second input must be the attention_rows node of dy";
+                const Node& y = g->nodes[rows.preds[1]];
+                if (y.preds != std::vector<int>(preds + 2, preds + n_preds) || y.p.heads != p.heads || y.p.kv_heads != p.kv_heads || y.p.scale != p.scale)
+                    return "attention backward: rows are of an attention with other inputs, heads or scale";
+            }
+            out = op == NG_OP_ATTENTION_DK || op == NG_OP_ATTENTION_DV ? k : q;
+            return nullptr;
+        }
+        case NG_OP_ATTENTION_ROWS: {
+            if (!need(2, 0)) return "attention_rows takes dy and y";
+            const Node& y = g->nodes[preds[1]];
+            if (y.op != NG_OP_ATTENTION || y.p.heads != p.heads) return "attention_rows: y must be an attention node with as many heads";
+            if (!(in(0) == in(1))) {
+                code = NG_ESHAPE;
+                return "attention_rows: dy and y differ in shape";
+            }
+            if (3 * p.heads * in(0).h * in(0).w > kMaxSliceElems || in(0).n * p.heads * ((in(0).h * in(0).w + 63) / 64) > kMaxAttentionTiles) {
+                code = NG_ESHAPE;
+                return "attention_rows: too many heads and queries";
+            }
+            out = in(0);
+            out.c = 3 * p.heads;
+            return nullptr;
+        }
         default:
             return "unknown operator kind";
     }
@@ -537,6 +612,21 @@ int ng_task_work(const ng_graph* g, int id, double* bytes, double* flops) {
         case NG_OP_GAP_DGRAD: b = 4 * (in0 + out); f = out; break;
         case NG_OP_CHANNEL_SUM: b = 4 * (in0 + out); f = in0; break;
         case NG_OP_SLICE_PAD: b = 4 * (out + out); break;
+        case NG_OP_HEAD_ROPE: b = 4 * (2 * out + (double)g->nodes[nd.preds[1]].out.elems()), f = 7 * out; break;
+        case NG_OP_HEAD_ROPE_DGRAD: b = 4 * ((nd.weights.size() > 1 ? 3 : 2) * out + (double)g->nodes[nd.preds[2]].out.elems()), f = 13 * out; break;
+        case NG_OP_HEAD_ROPE_WGRAD: b = 4 * (2 * in0 + (double)g->nodes[nd.preds[2]].out.elems() + out), f = 8 * in0; break;
+        case NG_OP_ATTENTION:
+        case NG_OP_ATTENTION_DQ:
+        case NG_OP_ATTENTION_DK:
+        case NG_OP_ATTENTION_DV: {                                  // products over every query and key: all there can be
+            const int first = nd.op == NG_OP_ATTENTION ? 0 : 2;
+            const Shape& k = g->nodes[nd.preds[first + 1]].out;
+            const double q = (double)g->nodes[nd.preds[first]].out.elems();
+            b = 4 * ((first ? 2 : 1) * q + 2 * (double)k.elems() + out);
+            f = 2 * q * (double)(k.h * k.w) * (nd.op == NG_OP_ATTENTION || nd.op == NG_OP_ATTENTION_DV ? 2 : 3);
+            break;
+        }
+        case NG_OP_ATTENTION_ROWS: b = 4 * (2 * in0 + out), f = 2 * in0; break;
         case NG_OP_SGD_UPDATE: b = 12.0 * nd.p.cout; f = 2.0 * nd.p.cout; break;
         default: break;
     }

@@ -1830,6 +1830,7 @@ __device__ __forceinline__ void dwconv_lds_tile(const DwArgs& a, int tile, float
 }
 
 #include "ng_train_tiles.inc"
+#include "ng_attention_tiles.inc"
 
 // ------------------------------------------------------------------------------------
 // kernel table: id -> argument type, tile function, name
@@ -1999,7 +2000,25 @@ NG_PAIR(KID_PAIR_DW_LDS, PairDwArgs, "dwconv_dgrad_lds+wgrad", KID_DW_DGRAD_LDS,
 #undef NG_PAIR
 NG_KERNEL(KID_PAIR_PW16, PairPwArgs, "conv1x1_px_dgrad+wgrad_16", pw_backward_tile < KID_PW_WGRAD_PX)
 NG_KERNEL(KID_PAIR_PW32, PairPwArgs, "conv1x1_px_dgrad+wgrad_32", pw_backward_tile < KID_PW_WGRAD_PX2)
+NG_KERNEL(KID_ROPE_4, RopeArgs, "head_rope_128", rope_tile < ROPE_FWD, 4)
+NG_KERNEL(KID_ROPE_8, RopeArgs, "head_rope_256", rope_tile < ROPE_FWD, 8)
+NG_KERNEL(KID_ROPE_N, RopeArgs, "head_rope_few", rope_few_tile < ROPE_FWD)
+NG_KERNEL(KID_ROPE_DX_4, RopeArgs, "head_rope_dgrad_128", rope_tile < ROPE_DX, 4)
+NG_KERNEL(KID_ROPE_DX_8, RopeArgs, "head_rope_dgrad_256", rope_tile < ROPE_DX, 8)
+NG_KERNEL(KID_ROPE_DX_N, RopeArgs, "head_rope_dgrad_few", rope_few_tile < ROPE_DX)
+NG_KERNEL(KID_ROPE_DG_4, RopeArgs, "head_rope_wgrad_128", rope_tile < ROPE_DG, 4)
+NG_KERNEL(KID_ROPE_DG_8, RopeArgs, "head_rope_wgrad_256", rope_tile < ROPE_DG, 8)
+NG_KERNEL(KID_ROPE_DG_N, RopeArgs, "head_rope_wgrad_few", rope_few_tile < ROPE_DG)
+NG_KERNEL(KID_ATTN_W64, AttnArgs, "attention_wave_64", attention_wave_tile < 4)
+NG_KERNEL(KID_ATTN_W128, AttnArgs, "attention_wave_128", attention_wave_tile < 8)
+NG_KERNEL(KID_ATTN_DQ_W64, AttnArgs, "attention_dq_wave_64", attention_dq_wave_tile < 4)
+NG_KERNEL(KID_ATTN_DQ_W128, AttnArgs, "attention_dq_wave_128", attention_dq_wave_tile < 8)
+NG_KERNEL(KID_ATTN_DK_W64, AttnArgs, "attention_dk_wave_64", attention_dkv_wave_tile < 4, true)
+NG_KERNEL(KID_ATTN_DK_W128, AttnArgs, "attention_dk_wave_128", attention_dkv_wave_tile < 8, true)
+NG_KERNEL(KID_ATTN_DV_W64, AttnArgs, "attention_dv_wave_64", attention_dkv_wave_tile < 4, false)
+NG_KERNEL(KID_ATTN_DV_W128, AttnArgs, "attention_dv_wave_128", attention_dkv_wave_tile < 8, false)
 #undef NG_KERNEL
+NG_KERNEL0(KID_ATTN_ROWS, AttnArgs, "attention_rows", attention_rows_tile)
 NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
 #undef NG_KERNEL0
 
@@ -2019,7 +2038,10 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_POOL_ROW_S1) X(KID_POOL_ROW_S2) X(KID_DW_LDS)                                                                               \
     X(KID_GEMM_PW_FWD) X(KID_GEMM_PW_DGRAD) X(KID_GEMM_PW_WGRAD) X(KID_GEMM_C3_FWD) X(KID_GEMM_C3_DGRAD)                \
     X(KID_GEMM_C3_WGRAD) X(KID_SMALL_GEMM) X(KID_PW_PX_FWD) X(KID_PW_PX_DGRAD) X(KID_PW_WGRAD_PX) X(KID_PW_WGRAD_PX2) X(KID_C3_WGRAD_PX) X(KID_C3_WGRAD_PX2) X(KID_BN_RAW) X(KID_BN_DGRAD) X(KID_BN_WGRAD) X(KID_RELU_DGRAD) X(KID_DW_DGRAD) X(KID_DW_DGRAD_LDS)                \
-    X(KID_DW_WGRAD) X(KID_POOL_DGRAD) X(KID_POOL_DGRAD_LDS) X(KID_GAP_DGRAD) X(KID_CHANNEL_SUM) X(KID_SLICE_PAD) X(KID_SGD) X(KID_SGD_BATCH) X(KID_BN_BACKWARD) X(KID_PAIR_DW) X(KID_PAIR_DW_LDS) X(KID_PAIR_PW16) X(KID_PAIR_PW32)
+    X(KID_DW_WGRAD) X(KID_POOL_DGRAD) X(KID_POOL_DGRAD_LDS) X(KID_GAP_DGRAD) X(KID_CHANNEL_SUM) X(KID_SLICE_PAD) X(KID_SGD) X(KID_SGD_BATCH) X(KID_BN_BACKWARD) X(KID_PAIR_DW) X(KID_PAIR_DW_LDS) X(KID_PAIR_PW16) X(KID_PAIR_PW32) \
+    X(KID_ROPE_4) X(KID_ROPE_8) X(KID_ROPE_N) X(KID_ROPE_DX_4) X(KID_ROPE_DX_8) X(KID_ROPE_DX_N) X(KID_ROPE_DG_4) X(KID_ROPE_DG_8) X(KID_ROPE_DG_N)    \
+    X(KID_ATTN_ROWS) X(KID_ATTN_W64) X(KID_ATTN_W128) X(KID_ATTN_DQ_W64) X(KID_ATTN_DQ_W128) X(KID_ATTN_DK_W64) X(KID_ATTN_DK_W128)    \
+    X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128)
 
 // A batch-norm epilogue is written into a task's argument block by type (C3Args or PwArgs, whose `ep` fields sit at
 // different offsets): the predicates that name the type must agree with the type the kernel takes.

@@ -1,9 +1,9 @@
-// The device-resident replay kernel. Compiled once per build of the kernel (NG_RESIDENT_BUILD: lean, full, train), each an
-// object of its own, so that the three compile side by side.
+// The device-resident replay kernel. Compiled once per build of the kernel (NG_RESIDENT_BUILD: lean, full, train, attention), each an
+// object of its own, so that they compile side by side.
 #include "ng_kernels.hip"
 
 #ifndef NG_RESIDENT_BUILD
-#error "compile with -DNG_RESIDENT_BUILD=0, 1 or 2"
+#error "compile with -DNG_RESIDENT_BUILD=0, 1, 2 or 3"
 #endif
 
 namespace ng {
@@ -162,7 +162,8 @@ struct CounterWait {
 
 // BUILD selects which tile functions are compiled in (see in_build): the lean build leaves out the kernels
 // that only large problems use - their register needs would otherwise shape the allocation of the whole
-// replay kernel -, the train build has the lean kernels plus those of graphs that train.
+// replay kernel -, the train build has the lean kernels plus those of graphs that train, the attention build the lean
+// kernels plus the attention kernels.
 template <int BUILD>
 __global__ __launch_bounds__(kGroup) void resident_kernel(DevPlan plan, unsigned epoch) {
     constexpr int kSmemPerSub = BUILD == BUILD_FULL ? kSmemFloatsWide : kSmemFloats;

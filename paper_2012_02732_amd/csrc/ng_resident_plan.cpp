@@ -112,6 +112,19 @@ double tile_round_us(const ng_graph* g, int v, int kid_any, int subs) {
             break;
         }
         case KID_BN_RAW: case KID_BN_DGRAD: case KID_RELU_DGRAD: case KID_GAP_DGRAD: case KID_SLICE_PAD: case KID_SGD: base = 1.2, per_tile = 0.15; break;
+        case KID_ROPE_4: case KID_ROPE_8: case KID_ROPE_DX_4: case KID_ROPE_DX_8: case KID_ROPE_DG_4: case KID_ROPE_DG_8: {
+            const RopeArgs* a = reinterpret_cast<const RopeArgs*>(g->tasks[v].args);
+            base = 3.0, per_tile = 0.01 * a->d * a->heads_per_tile * a->per_tile;    // 64 tokens of these heads through the memory pipeline
+            break;
+        }
+        case KID_ROPE_N: case KID_ROPE_DX_N: case KID_ROPE_DG_N: base = 2.0, per_tile = 0.3; break;
+        case KID_ATTN_ROWS: base = 3.0, per_tile = 0.3; break;
+        case KID_ATTN_W64: case KID_ATTN_W128: case KID_ATTN_DQ_W64: case KID_ATTN_DQ_W128: case KID_ATTN_DK_W64: case KID_ATTN_DK_W128:
+        case KID_ATTN_DV_W64: case KID_ATTN_DV_W128: {
+            const AttnArgs* a = reinterpret_cast<const AttnArgs*>(g->tasks[v].args);
+            base = 5.0, per_tile = 0.02 * a->d * (a->per_split / 4);                 // blocks of a wavefront: two or three products of 64 x 16 x d
+            break;
+        }
         case KID_DW_DGRAD: case KID_POOL_DGRAD: base = 2.0, per_tile = 0.7; break;
         case KID_POOL_DGRAD_LDS: case KID_DW_DGRAD_LDS: case KID_DW_LDS: base = 2.5, per_tile = 1.0; break;
         case KID_BN_WGRAD: case KID_CHANNEL_SUM: {

@@ -305,14 +305,22 @@ int build_resident(ng_graph* g) {
     NG_HIP(hipGetDevice(&dev));
     NG_HIP(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
     rt.resident_build = BUILD_LEAN;
+    bool attention = false;
+    for (const Task& t : g->tasks) attention = attention || (t.fn && is_attention_kernel(t.kid));
     for (const Task& t : g->tasks)
         if (t.fn && is_train_kernel(t.kid)) rt.resident_build = BUILD_TRAIN;
     for (const Task& t : g->tasks)
-        if (t.fn && !is_lean_kernel(t.kid) && !is_train_kernel(t.kid)) {
+        if (t.fn && !attention && !is_lean_kernel(t.kid) && !is_train_kernel(t.kid)) {
             if (rt.resident_build == BUILD_TRAIN && in_build(BUILD_TRAIN, t.kid)) continue;
             if (rt.resident_build == BUILD_TRAIN) return g->fail(NG_EINVAL, "device-resident replay: kernel %s does not belong in a graph that trains", t.name);
             rt.resident_build = BUILD_FULL;
         }
+    if (attention) {
+        // the attention build takes graphs of small tasks; others are replayed through the HIP graphs only
+        rt.resident_build = BUILD_ATTENTION;
+        for (const Task& t : g->tasks)
+            if (t.fn && !in_build(BUILD_ATTENTION, t.kid)) return NG_OK;
+    }
     NG_HIP(hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, resident_kernel_handle(rt.resident_build), kGroup, 0));
     if (per_cu < 1 || cus < 8) return g->fail(NG_EHIP, "device-resident replay: kernel does not fit (%d per CU, %d CUs)", per_cu, cus);
     per_cu = std::min(per_cu, g->resident_wg_per_cu > 0 ? g->resident_wg_per_cu : 1);   // one per CU: two slow each other's hand-overs down
@@ -529,7 +537,7 @@ int tune_resident(ng_graph* g) {
 
 int launch_resident(ng_graph* g) {
     Runtime& rt = *g->rt;
-    if (!rt.d_records) return g->fail(NG_ESTATE, "device-resident replay was not prepared");
+    if (!rt.d_records) return g->fail(NG_ESTATE, "device-resident replay: this graph has no plan (an attention operator next to a kernel for large problems or a graph that trains)");
     hipStream_t origin = rt.streams[0];
     if (rt.counters_dirty) {                                   // a timed-out replay left partial counts behind
         NG_HIP(hipStreamSynchronize(origin));
@@ -627,9 +635,11 @@ int ng_bind(ng_graph* g, void* arena, size_t arena_bytes, void* const* hip_strea
             if (int rc = pack_constants(g, v, rt.constants + const_off[v], rt.streams[0])) return rc;
         NG_HIP(hipStreamSynchronize(rt.streams[0]));
     }
+    g->packed_of.assign(g->nodes.size(), nullptr);
+    for (size_t v = 0; v < g->nodes.size() && rt.constants; ++v) g->packed_of[v] = rt.constants + const_off[v];
     g->tasks.assign(g->nodes.size(), Task());
     for (int v = 0; v < (int)g->nodes.size(); ++v)
-        if (int rc = build_task(g, v, rt.arena, rt.constants ? rt.constants + const_off[v] : nullptr, g->tasks[v])) return rc;
+        if (int rc = build_task(g, v, rt.arena, g->packed_of[v], g->tasks[v])) return rc;
     // Modes 0-3 run one kernel per task, with two exceptions (decide_launch_fusion): a batch-norm / ReLU
     // whose only input is a convolution result is applied by the convolution's kernel while the sums are
     // in registers (the same arithmetic on the same values; both tensors are stored), and a concat all of
@@ -747,7 +757,7 @@ int ng_capture(ng_graph* g) {
         const int saved = g->mode;
         for (int i = 0; i < 3; ++i) {
             g->auto_trial_us[i] = 0.f;
-            if (i == 0 && g->graph_multi_state != 1) continue;
+            if ((i == 0 && g->graph_multi_state != 1) || (i == 2 && !rt.d_records)) continue;
             g->mode = candidates[i];
             std::vector<float> us;
             for (int rep = 0; rep < 2 + 9; ++rep) {

@@ -288,8 +288,9 @@ void make_bn_backward_task(const Task& dgrad, const Task& wgrad, Task& t) {
 template <> const void* resident_build_handle<BUILD_LEAN>();
 template <> const void* resident_build_handle<BUILD_FULL>();
 template <> const void* resident_build_handle<BUILD_TRAIN>();
+template <> const void* resident_build_handle<BUILD_ATTENTION>();
 const void* resident_kernel_handle(int build) {
-    return build == BUILD_TRAIN ? resident_build_handle<BUILD_TRAIN>() : build == BUILD_FULL ? resident_build_handle<BUILD_FULL>() : resident_build_handle<BUILD_LEAN>();
+    return build == BUILD_ATTENTION ? resident_build_handle<BUILD_ATTENTION>() : build == BUILD_TRAIN ? resident_build_handle<BUILD_TRAIN>() : build == BUILD_FULL ? resident_build_handle<BUILD_FULL>() : resident_build_handle<BUILD_LEAN>();
 }
 
 namespace {
@@ -611,10 +612,92 @@ WgradPlan wgrad_plan(const ng_graph* g, int v) {
     }
     return p;
 }
+// How an attention node is computed: kernel, how the work is cut, and its share of the library-owned memory: workspace, then
+// arrival counters, then (forward, if somebody reads them) two numbers of every query.
+long round64(long n) { return (n + 63) & ~63L; }
+struct AttentionPlan {
+    int kid = KID_NONE;
+    int col_blocks = 1, splits = 1, per_split = 1;
+    long tiles = 0;
+    size_t ws_floats = 0, cnt_words = 0, stats_floats = 0;
+};
+bool is_attention_op(int op) { return op >= NG_OP_ATTENTION && op <= NG_OP_ATTENTION_DV; }
+AttentionPlan attention_plan(const ng_graph* g, int v) {
+    AttentionPlan p;
+    const Node& nd = g->nodes[v];
+    if (!is_attention_op(nd.op) || nd.op == NG_OP_ATTENTION_ROWS) return p;
+    const int first = nd.op == NG_OP_ATTENTION ? 0 : 2;
+    const Shape &q = g->nodes[nd.preds[first]].out, &k = g->nodes[nd.preds[first + 1]].out;
+    const long d = q.c / nd.p.heads, group = nd.p.heads / nd.p.kv_heads, Tq = q.h * q.w, Tk = k.h * k.w;
+    const bool by_keys = nd.op == NG_OP_ATTENTION_DK || nd.op == NG_OP_ATTENTION_DV;
+    const bool narrow = d <= 64;
+    p.kid = nd.op == NG_OP_ATTENTION ? (narrow ? KID_ATTN_W64 : KID_ATTN_W128) : nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_W64 : KID_ATTN_DQ_W128)
+          : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_W64 : KID_ATTN_DK_W128) : (narrow ? KID_ATTN_DV_W64 : KID_ATTN_DV_W128);
+    p.col_blocks = (int)ceil_div(by_keys ? Tk : group * Tq, 16);
+    const long groups = q.n * nd.p.kv_heads * p.col_blocks, blocks = by_keys ? group * ceil_div(Tq, 64) : ceil_div(Tk, 64);
+    // a split has a block for each of its four wavefronts at least
+    const long want = std::max<long>(1, std::min<long>(ceil_div(blocks, 4), ceil_div(1024, groups)));
+    p.per_split = (int)(ceil_div(ceil_div(blocks, want), 4) * 4);
+    p.splits = (int)ceil_div(blocks, p.per_split);
+    p.tiles = groups * p.splits;
+    if (p.splits > 1) {
+        p.ws_floats = (size_t)round64(p.tiles * (d + (nd.op == NG_OP_ATTENTION ? 2 : 0)) * 16);
+        p.cnt_words = (size_t)round64(groups);
+    }
+    if (nd.op == NG_OP_ATTENTION)
+        for (const Node& r : g->nodes)
+            if (r.op == NG_OP_ATTENTION_ROWS && r.preds[1] == v) p.stats_floats = (size_t)round64(2 * q.n * nd.p.heads * Tq);
+    return p;
+}
+struct RopePlan {
+    int kid = KID_NONE;
+    int blocks = 0, heads_per_tile = 1, items = 1, per_tile = 1;
+    long tiles = 0;
+    size_t ws_floats = 0, cnt_words = 0;
+};
+bool is_rope_op(int op) { return op >= NG_OP_HEAD_ROPE && op <= NG_OP_HEAD_ROPE_WGRAD; }
+RopePlan rope_plan(const ng_graph* g, int v) {
+    RopePlan p;
+    const Node& nd = g->nodes[v];
+    if (!is_rope_op(nd.op)) return p;
+    const int which = nd.op - NG_OP_HEAD_ROPE;                 // forward, dgrad, wgrad: in the order of the kernel ids
+    const Shape& x = g->nodes[nd.preds[which ? 1 : 0]].out;
+    const long d = x.c / nd.p.heads, T = x.h * x.w, H = nd.p.heads;
+    const bool wgrad = nd.op == NG_OP_HEAD_ROPE_WGRAD;
+    // workgroups: enough to fill the GPU; every one of wgrad's leaves a row of sums that somebody has to add up
+    const long most = wgrad ? 512 : 1L << 20;
+    if (T < 16) {
+        p.kid = KID_ROPE_N + 3 * which;
+        const long groups = ceil_div(x.n * H * T, 4);
+        p.per_tile = (int)ceil_div(groups, most);
+        p.tiles = ceil_div(groups, p.per_tile);
+    } else {
+        p.kid = (d <= 128 ? KID_ROPE_4 : KID_ROPE_8) + 3 * which;
+        p.blocks = (int)ceil_div(T, 64);
+        p.items = (int)(x.n * p.blocks);
+        p.heads_per_tile = (int)std::max<long>(1, std::min<long>(H, (long)p.items * H / (wgrad ? 512 : 1024)));
+        p.per_tile = (int)ceil_div(p.items, most);
+        p.tiles = ceil_div(p.items, p.per_tile) * ceil_div(H, p.heads_per_tile);
+    }
+    if (wgrad) {
+        const long groups = ceil_div(p.tiles, kGammaGroup);
+        p.ws_floats = (size_t)round64((p.tiles + groups) * d);
+        p.cnt_words = (size_t)round64(1 + groups);
+    }
+    return p;
+}
 }  // namespace
 
 size_t packed_floats(const ng_graph* g, int v) {
     const Node& nd = g->nodes[v];
+    if (is_attention_op(nd.op)) {
+        const AttentionPlan p = attention_plan(g, v);
+        return p.ws_floats + p.cnt_words + p.stats_floats;
+    }
+    if (is_rope_op(nd.op)) {
+        const RopePlan p = rope_plan(g, v);
+        return p.ws_floats + p.cnt_words;
+    }
     long wm, wn, wk;
     if (wgrad_dims(g, v, &wm, &wn, &wk)) {                     // split-K workspace: partial tiles, then the arrival counters
         const WgradPlan p = wgrad_plan(g, v);
@@ -640,6 +723,14 @@ size_t packed_floats(const ng_graph* g, int v) {
 int pack_constants(ng_graph* g, int v, float* packed, void* stream) {
     const Node& nd = g->nodes[v];
     long wm, wn, wk;
+    if (is_attention_op(nd.op) || is_rope_op(nd.op)) {         // the arrival counters start at zero
+        const AttentionPlan p = attention_plan(g, v);
+        const RopePlan r = rope_plan(g, v);
+        if (p.cnt_words + r.cnt_words == 0) return NG_OK;
+        const hipError_t e = hipMemsetAsync(packed + p.ws_floats + r.ws_floats, 0, (p.cnt_words + r.cnt_words) * sizeof(float), static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return g->fail(NG_EHIP, "clearing arrival counters of an attention operator: %s", hipGetErrorString(e));
+        return NG_OK;
+    }
     if (wgrad_dims(g, v, &wm, &wn, &wk)) {                     // the arrival counters start at zero
         const WgradPlan p = wgrad_plan(g, v);
         if (p.cnt_words == 0) return NG_OK;
@@ -695,6 +786,20 @@ int pack_constants(ng_graph* g, int v, float* packed, void* stream) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return g->fail(NG_EHIP, "repacking conv1x1 weights: %s", hipGetErrorString(e));
     return NG_OK;
+}
+
+// set_kernel for a kernel that a plan has chosen among those that take the same arguments
+template <class A>
+static void set_any_kernel(Task& t, int kid, const A& a, long ntiles) {
+    switch (kid) {
+#define NG_CASE(KID)                                                                             \
+    case KID:                                                                                    \
+        if constexpr (std::is_same<typename KernelOf<KID>::Args, A>::value) set_kernel<KID>(t, a, ntiles); \
+        break;
+        NG_FOR_EACH_KID(NG_CASE)
+#undef NG_CASE
+        default: break;
+    }
 }
 
 int build_task(ng_graph* g, int v, char* arena, float* packed, Task& t) {
@@ -1115,6 +1220,61 @@ int build_task(ng_graph* g, int v, char* arena, float* packed, Task& t) {
             a.g = buf(nd.preds[0]), a.flag = buf(v);
             a.lr = nd.p.lr, a.offset = nd.p.slice_lo[0], a.total = nd.p.cout;
             set_kernel<KID_SGD>(t, a, ceil_div(a.total, kBlock));
+            break;
+        }
+        case NG_OP_HEAD_ROPE:
+        case NG_OP_HEAD_ROPE_DGRAD:
+        case NG_OP_HEAD_ROPE_WGRAD: {
+            const RopePlan p = rope_plan(g, v);
+            const bool backward = nd.op != NG_OP_HEAD_ROPE, wgrad = nd.op == NG_OP_HEAD_ROPE_WGRAD;
+            const int first = backward ? 1 : 0;
+            const Shape &x = g->nodes[nd.preds[first]].out, &pos = g->nodes[nd.preds[first + 1]].out;
+            RopeArgs a{};
+            a.x = buf(nd.preds[first]), a.pos = buf(nd.preds[first + 1]);
+            if (backward) a.dy = buf(nd.preds[0]);
+            a.freq = wf(0), a.gamma = nd.weights.size() > 1 ? wf(1) : nullptr;
+            a.y = buf(v), a.dg = buf(v);
+            if (wgrad) {
+                if (!packed) return g->fail(NG_EINVAL, "node %d: no workspace", v);
+                a.ws = packed, a.cnt = reinterpret_cast<unsigned*>(packed + p.ws_floats);
+            }
+            a.eps = nd.p.eps, a.factor = nd.p.factor;
+            a.N = (int)x.n, a.H = nd.p.heads, a.d = (int)(x.c / nd.p.heads), a.T = (int)(x.h * x.w), a.rot = nd.p.rot, a.interleaved = nd.p.interleaved;
+            a.pos_stride = pos.n == 1 ? 0 : a.T;
+            a.blocks = p.blocks, a.heads_per_tile = p.heads_per_tile, a.items = p.items, a.per_tile = p.per_tile, a.tiles = (int)p.tiles;
+            set_any_kernel(t, p.kid, a, p.tiles);
+            break;
+        }
+        case NG_OP_ATTENTION_ROWS: {
+            const int y = nd.preds[1];
+            const Node& fwd = g->nodes[y];
+            const AttentionPlan p = attention_plan(g, y);
+            AttnArgs a{};
+            a.dy = buf(nd.preds[0]), a.q = buf(y), a.y = buf(v);
+            if (!g->packed_of.empty()) a.stats = g->packed_of[y] + p.ws_floats + p.cnt_words;
+            a.N = (int)fwd.out.n, a.H = fwd.p.heads, a.d = (int)(fwd.out.c / fwd.p.heads), a.Tq = (int)(fwd.out.h * fwd.out.w);
+            set_kernel<KID_ATTN_ROWS>(t, a, (long)a.N * a.H * ceil_div(a.Tq, 64));
+            break;
+        }
+        case NG_OP_ATTENTION:
+        case NG_OP_ATTENTION_DQ:
+        case NG_OP_ATTENTION_DK:
+        case NG_OP_ATTENTION_DV: {
+            const AttentionPlan p = attention_plan(g, v);
+            const int first = nd.op == NG_OP_ATTENTION ? 0 : 2;
+            const Shape &q = g->nodes[nd.preds[first]].out, &k = g->nodes[nd.preds[first + 1]].out;
+            AttnArgs a{};
+            a.q = buf(nd.preds[first]), a.k = buf(nd.preds[first + 1]), a.v = buf(nd.preds[first + 2]);
+            if ((int)nd.preds.size() == first + 4) a.len = buf(nd.preds[first + 3]);
+            if (first) a.dy = buf(nd.preds[0]), a.rows = buf(nd.preds[1]);
+            a.y = buf(v);
+            if (p.ws_floats + p.stats_floats > 0 && !packed) return g->fail(NG_EINVAL, "node %d: no workspace", v);
+            if (p.splits > 1) a.ws = packed, a.cnt = reinterpret_cast<unsigned*>(packed + p.ws_floats);
+            if (p.stats_floats > 0) a.stats = packed + p.ws_floats + p.cnt_words;
+            a.scale = nd.p.scale, a.scale_log2 = (float)((double)nd.p.scale * 1.4426950408889634074);
+            a.N = (int)q.n, a.H = nd.p.heads, a.Hk = nd.p.kv_heads, a.d = (int)(q.c / nd.p.heads), a.Tq = (int)(q.h * q.w), a.Tk = (int)(k.h * k.w);
+            a.col_blocks = p.col_blocks, a.splits = p.splits, a.per_split = p.per_split;
+            set_any_kernel(t, p.kid, a, p.tiles);
             break;
         }
         default:

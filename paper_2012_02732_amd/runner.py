@@ -56,7 +56,10 @@ _OPS = {"conv1x1": B.NG_OP_CONV1X1, "dwconv": B.NG_OP_DWCONV, "conv3x3": B.NG_OP
         "dwconv_dgrad": B.NG_OP_DWCONV_DGRAD, "dwconv_wgrad": B.NG_OP_DWCONV_WGRAD,
         "bn_act_dgrad": B.NG_OP_BN_ACT_DGRAD, "bn_act_wgrad": B.NG_OP_BN_ACT_WGRAD, "relu_dgrad": B.NG_OP_RELU_DGRAD,
         "pool_dgrad": B.NG_OP_POOL_DGRAD, "global_avgpool_dgrad": B.NG_OP_GAP_DGRAD, "channel_sum": B.NG_OP_CHANNEL_SUM,
-        "slice_pad": B.NG_OP_SLICE_PAD, "sgd_update": B.NG_OP_SGD_UPDATE}
+        "slice_pad": B.NG_OP_SLICE_PAD, "sgd_update": B.NG_OP_SGD_UPDATE,
+        "head_rope": B.NG_OP_HEAD_ROPE, "head_rope_dgrad": B.NG_OP_HEAD_ROPE_DGRAD, "head_rope_wgrad": B.NG_OP_HEAD_ROPE_WGRAD,
+        "attention": B.NG_OP_ATTENTION, "attention_rows": B.NG_OP_ATTENTION_ROWS, "attention_dq": B.NG_OP_ATTENTION_DQ,
+        "attention_dk": B.NG_OP_ATTENTION_DK, "attention_dv": B.NG_OP_ATTENTION_DV}
 
 
 def _params(nd) -> B.ng_op_params:
@@ -74,6 +77,9 @@ def _params(nd) -> B.ng_op_params:
         p.slice_lo[0], p.slice_hi[0], p.slice_lo[1] = int(q["src_lo"]), int(q["src_hi"]), int(q["dst_lo"])
     if nd.op == "sgd_update":
         p.lr, p.slice_lo[0], p.cout = float(q["lr"]), int(q["offset"]), int(q["numel"])
+    for name in ("heads", "kv_heads", "rot", "interleaved"):
+        setattr(p, name, int(q.get(name, 0)))
+    p.factor, p.scale = float(q.get("factor", 1.0)), float(q.get("scale", 0.0))
     return p
 
 
@@ -133,8 +139,10 @@ class GraphRunner:
         return B.ng_plan_memory(self.g)
 
     # -- GPU part ----------------------------------------------------------------
-    def prepare(self, resident_wg_per_cu=0, resident_xcds=0, resident_device_scope=0, plan_trials=None, launch_fusion=True):
-        """schedule -> plan -> bind -> capture, allocating arena and streams with torch."""
+    def prepare(self, resident_wg_per_cu=0, resident_xcds=0, resident_device_scope=0, plan_trials=None, launch_fusion=True,
+                origin_stream=None):
+        """schedule -> plan -> bind -> capture, allocating arena and streams with torch. ``origin_stream``: the handle of a
+        stream of the caller's (not the null stream) that replays are enqueued on, instead of one of this graph's own."""
         assert self.device is not None, "GraphRunner was created without a device"
         if plan_trials is not None:
             B.ng_resident_plan_trials(self.g, plan_trials)
@@ -146,15 +154,21 @@ class GraphRunner:
         nbytes = self.plan()
         self.arena = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
         base = (self.arena.data_ptr() + 255) // 256 * 256
+        if origin_stream == 0:
+            raise ValueError("the null stream cannot be captured: give a stream of its own")
         with torch.cuda.device(self.device):
-            self.streams = _new_streams(sched["n_streams"])
+            self.streams = _new_streams(sched["n_streams"] - (origin_stream is not None))
         torch.cuda.synchronize(self.device)
-        B.ng_bind(self.g, base, nbytes, self.streams)
+        B.ng_bind(self.g, base, nbytes, ([origin_stream] if origin_stream is not None else []) + self.streams)
         self.set_input(self.workload.input)
         for node_id, value in getattr(self.workload, "inputs", {}).items():
             self.set_input(value, node_id)
         B.ng_capture(self.g)
         return sched
+
+    def tensor(self, node_id) -> torch.Tensor:
+        """A node's tensor where it lies in the arena: the caller waits (``sync``) before reading it, and before writing an input."""
+        return self._view(node_id)
 
     def _view(self, node_id) -> torch.Tensor:
         shape = B.ng_node_shape(self.g, node_id)
@@ -162,8 +176,9 @@ class GraphRunner:
         n = int(np.prod(shape))
         return self.arena[off:off + 4 * n].view(torch.float32).view(*shape)
 
-    def set_input(self, x: np.ndarray, node_id: int = 0):
-        t = torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32))
+    def set_input(self, x, node_id: int = 0):
+        """Write an input tensor: a numpy array, or a torch tensor of any device."""
+        t = x if isinstance(x, torch.Tensor) else torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32))
         self._view(node_id).copy_(t.to(self.device))
         torch.cuda.synchronize(self.device)
 

@@ -9,7 +9,7 @@ own shape inference, scheduling and computation.
 Conventions shared by every consumer (an interface, not an implementation):
 
 * node ids are list positions; predecessors always have smaller ids, so the
-  ascending id order is a topological order (node 0 is the single input node);
+  ascending id order is a topological order (node 0 is an input node, the only one but for attention);
 * tensors are fp32, NCHW;
 * op vocabulary and parameters:
     input           n, c, h, w
@@ -27,7 +27,14 @@ Conventions shared by every consumer (an interface, not an implementation):
     global_avgpool  -                       -> [n, c, 1, 1]
     fc              cout                    weights: W[cout, cin], b[cout];
                                             input must be [n, cin, 1, 1]
+    head_rope       heads, rot, interleaved (0|1), eps, factor; preds x, positions [1 or n, 1, h, w]
+                                            weights: frequencies [rot / 2], and gamma [c / heads]: RMS norm
+                                            of each head (without gamma: none), then its first rot channels
+                                            rotated in pairs by position * frequency
+    attention       heads, kv_heads, scale; preds q, k, v and, if wanted, lengths [n, 1, 1, 1]: softmax
+                                            attention of q's h x w tokens to those of k and v, heads as runs
+                                            of channels, keys j < lengths[image] only
 """
-from .model import Node, Workload, OPS, TRAIN_OPS  # noqa: F401
+from .model import Builder, Node, Workload, OPS, ATTENTION_OPS, TRAIN_OPS, rope_frequencies  # noqa: F401
 from .configs import make, CONFIG_NAMES  # noqa: F401
 from .training import training_graph, nas_cell_cifar, TrainingWorkload  # noqa: F401

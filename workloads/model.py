@@ -8,10 +8,12 @@ import numpy as np
 
 OPS = ("input", "conv1x1", "dwconv", "conv3x3", "bn_act", "relu", "add_n",
        "concat", "pool", "global_avgpool", "fc")
+ATTENTION_OPS = ("head_rope", "attention")
 # operators that only occur in the DAG of a training iteration (see workloads/training.py)
 TRAIN_OPS = ("conv1x1_dgrad", "conv1x1_wgrad", "conv3x3_dgrad", "conv3x3_wgrad", "dwconv_dgrad", "dwconv_wgrad",
              "bn_act_dgrad", "bn_act_wgrad", "relu_dgrad", "pool_dgrad", "global_avgpool_dgrad", "channel_sum",
-             "slice_pad", "sgd_update")
+             "slice_pad", "sgd_update", "head_rope_dgrad", "head_rope_wgrad",
+             "attention_rows", "attention_dq", "attention_dk", "attention_dv")
 
 
 @dataclass
@@ -36,6 +38,7 @@ class Workload:
     nodes: List[Node]
     input: np.ndarray          # fp32 [n, c, h, w], the value of node 0
     outputs: List[int]         # ids whose tensors are compared / returned
+    inputs: Dict[int, np.ndarray] = field(default_factory=dict)      # values of the input nodes (of those other than node 0, if there are any)
 
     @property
     def edges(self) -> List[Tuple[int, int]]:
@@ -45,6 +48,18 @@ class Workload:
 
 def _out_hw(h: int, w: int, k: int, stride: int, pad: int) -> Tuple[int, int]:
     return (h + 2 * pad - k) // stride + 1, (w + 2 * pad - k) // stride + 1
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0) -> np.ndarray:
+    """Angle per position of each of the rot / 2 rotated pairs, base^(-2 i / rot). For contexts ``factor`` times as long as the
+    network was trained on: "linear" turns every pair that much slower, "ntk" raises the base so that the slowest pair does and the
+    fastest keeps its pace."""
+    if scaling not in ("none", "linear", "ntk"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if scaling == "ntk" and rot > 2:
+        base = base * factor ** (rot / (rot - 2.0))
+    f = base ** (-np.arange(0, rot, 2, dtype=np.float64) / rot)
+    return (f / factor if scaling == "linear" else f).astype(np.float32)
 
 
 class Builder:
@@ -67,7 +82,6 @@ class Builder:
         return self.nodes[i].shape
 
     def input(self, n, c, h, w) -> int:
-        assert not self.nodes
         return self._add("input", [], (n, c, h, w), n=n, c=c, h=h, w=w)
 
     def conv1x1(self, x, cout, init_gain: float = 1.0) -> int:
@@ -125,6 +139,25 @@ class Builder:
         assert h == 1 and w == 1
         return self._add("fc", [x], (n, cout, 1, 1), cout=cout)
 
+    def head_rope(self, x, positions, heads, frequencies, norm=True, interleaved=False, eps=1e-6, factor=1.0) -> int:
+        """Norm of each head (``norm``) and its rotation by the token's position (see ``rope_frequencies``)."""
+        n, c, h, w = self.shape(x)
+        assert c % heads == 0 and self.shape(positions) in ((1, 1, h, w), (n, 1, h, w))
+        freq = np.ascontiguousarray(frequencies, dtype=np.float32)
+        v = self._add("head_rope", [x, positions], (n, c, h, w), heads=heads, rot=2 * len(freq), interleaved=int(bool(interleaved)),
+                      eps=float(eps), factor=float(factor))
+        self.nodes[v].weights = [freq] + ([np.ones(c // heads, np.float32)] if norm else [])
+        return v
+
+    def attention(self, q, k, v, heads, kv_heads=None, lengths=None, scale=None) -> int:
+        """Attention of q's tokens to the tokens of k and v; lengths [n, 1, 1, 1]: keys that count for each image."""
+        n, c, h, w = self.shape(q)
+        kv_heads = heads if kv_heads is None else kv_heads
+        assert c % heads == 0 and self.shape(k) == self.shape(v) and self.shape(k)[:2] == (n, c // heads * kv_heads)
+        preds = [q, k, v] + ([] if lengths is None else [lengths])
+        return self._add("attention", preds, (n, c, h, w), heads=heads, kv_heads=kv_heads,
+                         scale=float((c // heads) ** -0.5 if scale is None else scale))
+
     # -- values --------------------------------------------------------
     def draw_weights(self, rng: np.random.Generator, conv_std, bn_mode: str):
         """Fill weights in ascending node id.
@@ -151,6 +184,9 @@ class Builder:
                 cin = self.shape(nd.preds[0])[1]
                 nd.weights = [normal((nd.params["cout"], cin), cin),
                               (rng.standard_normal(nd.params["cout"]) * 0.01).astype(np.float32)]
+            elif nd.op == "head_rope" and len(nd.weights) > 1:
+                if bn_mode != "identity":
+                    nd.weights[1] = rng.uniform(0.8, 1.2, nd.weights[1].shape).astype(np.float32)
             elif nd.op == "bn_act":
                 c = nd.shape[1]
                 if bn_mode == "identity":

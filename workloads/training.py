@@ -19,6 +19,9 @@ forward operator's input; weights are shared with the forward node):
     bn_act_dgrad / _wgrad  preds [dy, x]   eps, relu                      shared gamma, beta, mean, var; wgrad -> [2, c, 1, 1]
     relu_dgrad, pool_dgrad (mode, stride, pad), global_avgpool_dgrad      preds [dy, x]
     channel_sum           preds [dy]                                      -> [1, c, 1, 1]  (fc bias gradient)
+    head_rope_dgrad / _wgrad preds [dy, x, positions]  the forward's parameters  shared frequencies, gamma; wgrad -> [1, d, 1, 1]
+    attention_rows        preds [dy, y]    heads                           -> [n, 3 heads, h, w]
+    attention_dq / _dk / _dv preds [dy, rows, q, k, v(, lengths)]  heads, kv_heads, scale
     slice_pad             preds [dy]       cout, src_lo, src_hi, dst_lo   (gradient of one concat input)
     sgd_update            preds [grad, the other readers of the weight: its backward operator, its forward node]
                           lr, offset, numel                                shared W (written in place)
@@ -38,7 +41,6 @@ from .model import Node, Workload
 class TrainingWorkload(Workload):
     forward: Workload = None
     lr: float = 0.0
-    inputs: Dict[int, np.ndarray] = field(default_factory=dict)      # input node id -> value (x and the seeds)
     seed_of: Dict[int, int] = field(default_factory=dict)            # forward output -> its seed input node
     grad_of: Dict[int, int] = field(default_factory=dict)            # forward node -> node holding dL/d(its value)
     wgrad_of: Dict[Tuple[int, int], Tuple[int, int, int]] = field(default_factory=dict)   # (forward node, weight j) -> (node, offset, numel)
@@ -53,7 +55,7 @@ def training_graph(fwd: Workload, lr: float, seeds: Dict[int, np.ndarray]) -> Tr
         nodes.append(Node(op, list(preds), dict(params), [], tuple(int(s) for s in shape), 1.0, list(shared)))
         return len(nodes) - 1
 
-    inputs = {0: fwd.input}
+    inputs = {0: fwd.input, **fwd.inputs}                   # and the seeds
     seed_of, grad_of, wgrad_of, update_of = {}, {}, {}, {}
     contrib: Dict[int, List[int]] = {v: [] for v in range(n_fwd)}
     for o in sorted(seeds):
@@ -113,6 +115,23 @@ def training_graph(fwd: Workload, lr: float, seeds: Dict[int, np.ndarray]) -> Tr
             update(v, 1, wg, xs[1], xs[1], [dx])            # beta
             if want_dx:
                 contrib[x].append(dx)
+        elif nd.op == "head_rope":
+            pos, shared = nd.preds[1], [(v, j) for j in range(len(nd.weights))]
+            how = {k: p[k] for k in ("heads", "rot", "interleaved", "eps", "factor")}
+            dx = add("head_rope_dgrad", [dy, x, pos], xs, shared=shared, **how) if want_dx else None
+            if len(nd.weights) > 1:
+                wg = add("head_rope_wgrad", [dy, x, pos], (1, xs[1] // p["heads"], 1, 1), shared=shared, **how)
+                update(v, 1, wg, 0, xs[1] // p["heads"], [dx])
+            if want_dx:
+                contrib[x].append(dx)
+        elif nd.op == "attention":
+            if not any(needs_grad[u] for u in nd.preds[:3]):
+                continue
+            how = {k: p[k] for k in ("heads", "kv_heads", "scale")}
+            rows = add("attention_rows", [dy, v], (nd.shape[0], 3 * p["heads"]) + tuple(nd.shape[2:]), heads=p["heads"])
+            for u, op in zip(nd.preds, ("attention_dq", "attention_dk", "attention_dv")):
+                if needs_grad[u]:
+                    contrib[u].append(add(op, [dy, rows] + nd.preds, fwd.nodes[u].shape, **how))
         elif nd.op == "relu":
             if want_dx:
                 contrib[x].append(add("relu_dgrad", [dy, x], xs))
