@@ -103,8 +103,9 @@ constexpr int kSmemFloats = 5120;
 // ... and what the patch-stationary kernels get instead: 24 floats (16 channels in three bf16 parts) for every pixel of their patches,
 // 640 at most. Stand-alone kernels: only they; the resident kernel: every workgroup of the build that contains them.
 constexpr int kSmemFloatsPatch = 24 * 256, kSmemFloatsWide = 24 * 640;
+constexpr int attention_tile_floats(int kid);                  // ng_attention_tiles.inc
 constexpr int smem_floats(int kid) {
-    return is_c3_patch(kid) ? 24 * c3_patches(kid) * c3_patch_pixels(kid) : kid == KID_PW_P32 ? 2 * kSmemFloatsPatch : is_pw_patch(kid) ? kSmemFloatsPatch : kSmemFloats;
+    return is_attention_tile_kernel(kid) ? attention_tile_floats(kid) : is_c3_patch(kid) ? 24 * c3_patches(kid) * c3_patch_pixels(kid) : kid == KID_PW_P32 ? 2 * kSmemFloatsPatch : is_pw_patch(kid) ? kSmemFloatsPatch : kSmemFloats;
 }
 
 // ------------------------------------------------------------------------------------
@@ -2017,6 +2018,8 @@ NG_KERNEL(KID_ATTN_DK_W64, AttnArgs, "attention_dk_wave_64", attention_dkv_wave_
 NG_KERNEL(KID_ATTN_DK_W128, AttnArgs, "attention_dk_wave_128", attention_dkv_wave_tile < 8, true)
 NG_KERNEL(KID_ATTN_DV_W64, AttnArgs, "attention_dv_wave_64", attention_dkv_wave_tile < 4, false)
 NG_KERNEL(KID_ATTN_DV_W128, AttnArgs, "attention_dv_wave_128", attention_dkv_wave_tile < 8, false)
+NG_KERNEL(KID_ATTN_T64, AttnArgs, "attention_tile_64", attention_tile < 64)
+NG_KERNEL(KID_ATTN_T128, AttnArgs, "attention_tile_128", attention_tile < 128)
 #undef NG_KERNEL
 NG_KERNEL0(KID_ATTN_ROWS, AttnArgs, "attention_rows", attention_rows_tile)
 NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
@@ -2041,7 +2044,7 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_DW_WGRAD) X(KID_POOL_DGRAD) X(KID_POOL_DGRAD_LDS) X(KID_GAP_DGRAD) X(KID_CHANNEL_SUM) X(KID_SLICE_PAD) X(KID_SGD) X(KID_SGD_BATCH) X(KID_BN_BACKWARD) X(KID_PAIR_DW) X(KID_PAIR_DW_LDS) X(KID_PAIR_PW16) X(KID_PAIR_PW32) \
     X(KID_ROPE_4) X(KID_ROPE_8) X(KID_ROPE_N) X(KID_ROPE_DX_4) X(KID_ROPE_DX_8) X(KID_ROPE_DX_N) X(KID_ROPE_DG_4) X(KID_ROPE_DG_8) X(KID_ROPE_DG_N)    \
     X(KID_ATTN_ROWS) X(KID_ATTN_W64) X(KID_ATTN_W128) X(KID_ATTN_DQ_W64) X(KID_ATTN_DQ_W128) X(KID_ATTN_DK_W64) X(KID_ATTN_DK_W128)    \
-    X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128)
+    X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128) X(KID_ATTN_T64) X(KID_ATTN_T128)
 
 // A batch-norm epilogue is written into a task's argument block by type (C3Args or PwArgs, whose `ep` fields sit at
 // different offsets): the predicates that name the type must agree with the type the kernel takes.

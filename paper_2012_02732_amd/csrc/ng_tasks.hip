@@ -633,15 +633,20 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     const bool narrow = d <= 64;
     p.kid = nd.op == NG_OP_ATTENTION ? (narrow ? KID_ATTN_W64 : KID_ATTN_W128) : nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_W64 : KID_ATTN_DQ_W128)
           : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_W64 : KID_ATTN_DK_W128) : (narrow ? KID_ATTN_DV_W64 : KID_ATTN_DV_W128);
-    p.col_blocks = (int)ceil_div(by_keys ? Tk : group * Tq, 16);
-    const long groups = q.n * nd.p.kv_heads * p.col_blocks, blocks = by_keys ? group * ceil_div(Tq, 64) : ceil_div(Tk, 64);
-    // a split has a block for each of its four wavefronts at least
-    const long want = std::max<long>(1, std::min<long>(ceil_div(blocks, 4), ceil_div(1024, groups)));
-    p.per_split = (int)(ceil_div(ceil_div(blocks, want), 4) * 4);
+    const long columns = by_keys ? Tk : group * Tq;
+    long per_block = 16, other = 64, few = 4, workgroups = 1024;   // columns of a workgroup, the other side's in a block, blocks a split has at least
+    if (nd.op == NG_OP_ATTENTION && columns > 32) {
+        p.kid = narrow ? KID_ATTN_T64 : KID_ATTN_T128;
+        per_block = kAttentionColumns, other = narrow ? attention_block<64>() : attention_block<128>(), few = 2, workgroups = 512;
+    }
+    p.col_blocks = (int)ceil_div(columns, per_block);
+    const long groups = q.n * nd.p.kv_heads * p.col_blocks, blocks = by_keys ? group * ceil_div(Tq, other) : ceil_div(Tk, other);
+    const long want = std::max<long>(1, std::min<long>(ceil_div(blocks, few), ceil_div(workgroups, groups)));
+    p.per_split = (int)(ceil_div(ceil_div(blocks, want), few) * few);
     p.splits = (int)ceil_div(blocks, p.per_split);
     p.tiles = groups * p.splits;
     if (p.splits > 1) {
-        p.ws_floats = (size_t)round64(p.tiles * (d + (nd.op == NG_OP_ATTENTION ? 2 : 0)) * 16);
+        p.ws_floats = (size_t)round64(p.tiles * (d + (nd.op == NG_OP_ATTENTION ? 2 : 0)) * per_block);
         p.cnt_words = (size_t)round64(groups);
     }
     if (nd.op == NG_OP_ATTENTION)

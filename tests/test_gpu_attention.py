@@ -118,6 +118,11 @@ ATTENTION = [                   # n, heads, kv_heads, d, Tq, Tk, lengths
     (1, 1, 1, 33, 700, 1, None),
     (2, 6, 2, 64, 257, 333, "ragged"),
     (1, 4, 4, 128, 300, 520, None),
+    (2, 2, 2, 128, 129, 1, None),
+    (3, 3, 1, 48, 43, 97, "ragged"),
+    (1, 1, 1, 128, 40, 2050, None),
+    (4, 2, 2, 64, 64, 3000, "ragged"),
+    (1, 8, 2, 96, 33, 31, None),
 ]
 
 
