@@ -2020,6 +2020,12 @@ NG_KERNEL(KID_ATTN_DV_W64, AttnArgs, "attention_dv_wave_64", attention_dkv_wave_
 NG_KERNEL(KID_ATTN_DV_W128, AttnArgs, "attention_dv_wave_128", attention_dkv_wave_tile < 8, false)
 NG_KERNEL(KID_ATTN_T64, AttnArgs, "attention_tile_64", attention_tile < 64)
 NG_KERNEL(KID_ATTN_T128, AttnArgs, "attention_tile_128", attention_tile < 128)
+NG_KERNEL(KID_ATTN_DQ_T64, AttnArgs, "attention_dq_tile_64", attention_dq_tile < 64)
+NG_KERNEL(KID_ATTN_DQ_T128, AttnArgs, "attention_dq_tile_128", attention_dq_tile < 128)
+NG_KERNEL(KID_ATTN_DK_T64, AttnArgs, "attention_dk_tile_64", attention_dk_tile < 64)
+NG_KERNEL(KID_ATTN_DK_T128, AttnArgs, "attention_dk_tile_128", attention_dk_tile < 128)
+NG_KERNEL(KID_ATTN_DV_T64, AttnArgs, "attention_dv_tile_64", attention_dv_tile < 64)
+NG_KERNEL(KID_ATTN_DV_T128, AttnArgs, "attention_dv_tile_128", attention_dv_tile < 128)
 #undef NG_KERNEL
 NG_KERNEL0(KID_ATTN_ROWS, AttnArgs, "attention_rows", attention_rows_tile)
 NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
@@ -2044,7 +2050,8 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_DW_WGRAD) X(KID_POOL_DGRAD) X(KID_POOL_DGRAD_LDS) X(KID_GAP_DGRAD) X(KID_CHANNEL_SUM) X(KID_SLICE_PAD) X(KID_SGD) X(KID_SGD_BATCH) X(KID_BN_BACKWARD) X(KID_PAIR_DW) X(KID_PAIR_DW_LDS) X(KID_PAIR_PW16) X(KID_PAIR_PW32) \
     X(KID_ROPE_4) X(KID_ROPE_8) X(KID_ROPE_N) X(KID_ROPE_DX_4) X(KID_ROPE_DX_8) X(KID_ROPE_DX_N) X(KID_ROPE_DG_4) X(KID_ROPE_DG_8) X(KID_ROPE_DG_N)    \
     X(KID_ATTN_ROWS) X(KID_ATTN_W64) X(KID_ATTN_W128) X(KID_ATTN_DQ_W64) X(KID_ATTN_DQ_W128) X(KID_ATTN_DK_W64) X(KID_ATTN_DK_W128)    \
-    X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128) X(KID_ATTN_T64) X(KID_ATTN_T128)
+    X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128) X(KID_ATTN_T64) X(KID_ATTN_T128) X(KID_ATTN_DQ_T64) X(KID_ATTN_DQ_T128)    \
+    X(KID_ATTN_DK_T64) X(KID_ATTN_DK_T128) X(KID_ATTN_DV_T64) X(KID_ATTN_DV_T128)
 
 // A batch-norm epilogue is written into a task's argument block by type (C3Args or PwArgs, whose `ep` fields sit at
 // different offsets): the predicates that name the type must agree with the type the kernel takes.

@@ -638,6 +638,10 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     if (nd.op == NG_OP_ATTENTION && columns > 32) {
         p.kid = narrow ? KID_ATTN_T64 : KID_ATTN_T128;
         per_block = kAttentionColumns, other = narrow ? attention_block<64>() : attention_block<128>(), few = 2, workgroups = 512;
+    } else if (nd.op != NG_OP_ATTENTION && columns > 32) {
+        p.kid = nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_T64 : KID_ATTN_DQ_T128) : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_T64 : KID_ATTN_DK_T128)
+              : (narrow ? KID_ATTN_DV_T64 : KID_ATTN_DV_T128);
+        per_block = kAttentionColumns, other = kGradientBlock, few = 2, workgroups = narrow ? 512 : 256;
     }
     p.col_blocks = (int)ceil_div(columns, per_block);
     const long groups = q.n * nd.p.kv_heads * p.col_blocks, blocks = by_keys ? group * ceil_div(Tq, other) : ceil_div(Tk, other);
