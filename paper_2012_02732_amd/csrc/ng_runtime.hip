@@ -106,6 +106,12 @@ int issue_all(ng_graph* g, bool multi) {
     return NG_OK;
 }
 
+// A single-stream record of at most this many launches is replayed launch by launch: the same kernels and arguments in the same
+// order on the same stream. A graph launch takes the host 16 us however short the record is, a kernel launch 2.7 us. Chains of small
+// kernels, us a replay by graph launch and launch by launch, one after the other: 1 kernel 16.3 and 3.0, 4 17.7 and 11.0, 6 18.4 and
+// 16.0, 8 20.9 and 21.5; each awaited: 39.0 and 14.4, 39.3 and 19.9, 40.9 and 23.9, 42.4 and 56.7.
+constexpr size_t kDirectLaunches = 6;
+
 // Single-stream record: pre-run the task table on the origin stream under stream capture.
 int capture_single(ng_graph* g, int slot) {
     Runtime& rt = *g->rt;
@@ -854,7 +860,10 @@ int ng_replay(ng_graph* g) {
                                           "(%d replays compared); choose another replay mode", g->graph_multi_checked);
             NG_HIP(hipGraphLaunch(rt.exec[0], rt.streams[0]));
             return NG_OK;
-        case NG_MODE_GRAPH_SINGLE: NG_HIP(hipGraphLaunch(rt.exec[1], rt.streams[0])); return NG_OK;
+        case NG_MODE_GRAPH_SINGLE:
+            if (g->single_launches.size() <= kDirectLaunches) return issue_all(g, false);
+            NG_HIP(hipGraphLaunch(rt.exec[1], rt.streams[0]));
+            return NG_OK;
         case NG_MODE_EAGER_SINGLE: return issue_all(g, false);
         case NG_MODE_EAGER_MULTI: return issue_all(g, true);
         default: return launch_resident(g);
