@@ -231,7 +231,8 @@ int ng_set_memory_reuse(ng_graph* g, int on);
  * and x) are computed in one walk over dy and x by the launch of whichever of the two comes first, if
  * both are on one stream (always, in modes 1 and 2); likewise the input gradient and the weight gradient
  * of a depthwise or 1 x 1 convolution (same dy) share one launch, their workgroups interleaved, if
- * everything the later one reads is complete when the earlier one starts. In modes 1 and 2 tasks of the
+ * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, and dk and
+ * dv of an attention with many keys and heads of up to 64 channels, with what both need computed once. In modes 1 and 2 tasks of the
  * same kernel that do not wait for each other share a launch as well, and the launches follow each other in an
  * order that lets them (ng_get_single_launches). on = 0 switches the exceptions off: one kernel per task. Call before ng_bind (NG_ESTATE after). */
 int ng_set_launch_fusion(ng_graph* g, int on);
@@ -310,7 +311,8 @@ enum {
                                  with the single-stream graph's result (ng_graph_multi_check); if they ever differ
                                  the mode is not a candidate of NG_MODE_AUTO and ng_replay refuses it (NG_ESTATE).
                                  The check is a screen, not a proof: rare misorderings can pass it. */
-    NG_MODE_GRAPH_SINGLE = 1, /* captured single-stream graph */
+    NG_MODE_GRAPH_SINGLE = 1, /* captured single-stream graph (a record of six launches or fewer: launched one by one, which takes less than
+                                 a graph launch; the same kernels in the same order) */
     NG_MODE_EAGER_SINGLE = 2, /* task table launched kernel by kernel on the origin stream */
     NG_MODE_EAGER_MULTI = 3,  /* task table launched on the assigned streams with real events */
     NG_MODE_DEVICE_RESIDENT = 4, /* one launch; persistent workgroups walk the recorded schedule themselves:

@@ -55,10 +55,13 @@ enum Kid : int {
     // a wavefront owns 16 queries (DK, DV: 16 keys) of heads of up to 64 / 128 channels and reads its operands straight from memory
     KID_ATTN_W64, KID_ATTN_W128, KID_ATTN_DQ_W64, KID_ATTN_DQ_W128, KID_ATTN_DK_W64, KID_ATTN_DK_W128, KID_ATTN_DV_W64, KID_ATTN_DV_W128,
     // the same for many columns: 128 for each workgroup, the other side staged through LDS (launched kernels only)
-    KID_ATTN_T64, KID_ATTN_T128, KID_ATTN_DQ_T64, KID_ATTN_DQ_T128, KID_ATTN_DK_T64, KID_ATTN_DK_T128, KID_ATTN_DV_T64, KID_ATTN_DV_T128,
+    KID_ATTN_T64, KID_ATTN_T128, KID_ATTN_DQ_T64, KID_ATTN_DQ_T128, KID_ATTN_DK_T64, KID_ATTN_DK_T128, KID_ATTN_DV_T64, KID_ATTN_DV_T128, KID_ATTN_DKV_T64,
+    // both gradients of norm and rotation in one launch (launched kernels only)
+    KID_ROPE_BOTH_4, KID_ROPE_BOTH_8, KID_ROPE_BOTH_N,
     KID_COUNT
 };
-constexpr bool is_attention_tile_kernel(int kid) { return kid >= KID_ATTN_T64 && kid < KID_COUNT; }
+constexpr bool is_attention_tile_kernel(int kid) { return kid >= KID_ATTN_T64 && kid <= KID_ATTN_DKV_T64; }
+constexpr bool is_launched_attention_kernel(int kid) { return kid >= KID_ATTN_T64 && kid < KID_COUNT; }
 constexpr bool is_attention_kernel(int kid) { return kid >= KID_ROPE_4 && kid < KID_COUNT; }
 constexpr bool is_train_kernel(int kid) { return kid >= KID_GEMM_PW_FWD && kid <= KID_SGD; }
 
@@ -85,10 +88,7 @@ constexpr bool is_c3_patch(int kid) { return kid >= KID_C3_P64 && kid <= KID_C3_
 constexpr int c3_patches(int kid) { return kid == KID_C3_SK ? 4 : kid == KID_C3_P64 || kid == KID_C3_P96 || kid == KID_C3_Q32 ? 2 : 1; }
 constexpr int c3_patch_pixels(int kid) { return kid == KID_C3_SK ? 160 : kid == KID_C3_Q64 ? 384 : kid == KID_C3_R32 || kid == KID_C3_R128 ? 640 : 256; }
 // wavefronts per SIMD that the registers of a stand-alone kernel must leave room for: the compiler takes more than half of them for 96 rows
-// (the attention gradients of 128 channels a head take nearly all of them)
-constexpr int min_waves(int kid) {
-    return (is_c3_patch(kid) && kid != KID_C3_SK) || (is_attention_tile_kernel(kid) && kid != KID_ATTN_DQ_T128 && kid != KID_ATTN_DK_T128) ? 2 : 1;
-}
+constexpr int min_waves(int kid) { return (is_c3_patch(kid) && kid != KID_C3_SK) || is_attention_tile_kernel(kid) ? 2 : 1; }
 constexpr bool is_pw_columns(int kid) { return (kid >= KID_PW_V1 && kid <= KID_PW_S4) || kid == KID_PW_P32 || kid == KID_PW_P64; }   // tiles = row tiles x column blocks
 constexpr bool is_pw_patch(int kid) { return kid == KID_PW_P32 || kid == KID_PW_P64; }
 // windowed kernels for large tensors (batches): not in the lean build, but in the full and the train build
@@ -137,7 +137,7 @@ constexpr bool is_lean_kernel(int kid) {
 // too large to gain from this mode).
 enum { BUILD_LEAN = 0, BUILD_FULL = 1, BUILD_TRAIN = 2, BUILD_ATTENTION = 3 };
 constexpr bool in_build(int build, int kid) {
-    return (kid >= KID_SGD_BATCH && kid <= KID_PAIR_PW32) ? false : build == BUILD_ATTENTION ? is_lean_kernel(kid) || (is_attention_kernel(kid) && !is_attention_tile_kernel(kid)) : is_attention_kernel(kid) ? false : build == BUILD_LEAN ? is_lean_kernel(kid) : build == BUILD_FULL ? !is_train_kernel(kid) : (is_lean_kernel(kid) || is_train_kernel(kid) || is_large_tensor_kernel(kid));
+    return (kid >= KID_SGD_BATCH && kid <= KID_PAIR_PW32) ? false : build == BUILD_ATTENTION ? is_lean_kernel(kid) || (is_attention_kernel(kid) && !is_launched_attention_kernel(kid)) : is_attention_kernel(kid) ? false : build == BUILD_LEAN ? is_lean_kernel(kid) : build == BUILD_FULL ? !is_train_kernel(kid) : (is_lean_kernel(kid) || is_train_kernel(kid) || is_large_tensor_kernel(kid));
 }
 
 constexpr int kBlock = 256;          // threads that work on one tile (a stand-alone kernel's workgroup)

@@ -2026,6 +2026,10 @@ NG_KERNEL(KID_ATTN_DK_T64, AttnArgs, "attention_dk_tile_64", attention_dk_tile <
 NG_KERNEL(KID_ATTN_DK_T128, AttnArgs, "attention_dk_tile_128", attention_dk_tile < 128)
 NG_KERNEL(KID_ATTN_DV_T64, AttnArgs, "attention_dv_tile_64", attention_dv_tile < 64)
 NG_KERNEL(KID_ATTN_DV_T128, AttnArgs, "attention_dv_tile_128", attention_dv_tile < 128)
+NG_KERNEL(KID_ATTN_DKV_T64, PairAttnArgs, "attention_dk+dv_tile_64", attention_dk_dv_tile < 64)
+NG_KERNEL(KID_ROPE_BOTH_4, RopeArgs, "head_rope_dgrad+wgrad_128", rope_tile < ROPE_BOTH, 4)
+NG_KERNEL(KID_ROPE_BOTH_8, RopeArgs, "head_rope_dgrad+wgrad_256", rope_tile < ROPE_BOTH, 8)
+NG_KERNEL(KID_ROPE_BOTH_N, RopeArgs, "head_rope_dgrad+wgrad_few", rope_few_tile < ROPE_BOTH)
 #undef NG_KERNEL
 NG_KERNEL0(KID_ATTN_ROWS, AttnArgs, "attention_rows", attention_rows_tile)
 NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
@@ -2051,7 +2055,8 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_ROPE_4) X(KID_ROPE_8) X(KID_ROPE_N) X(KID_ROPE_DX_4) X(KID_ROPE_DX_8) X(KID_ROPE_DX_N) X(KID_ROPE_DG_4) X(KID_ROPE_DG_8) X(KID_ROPE_DG_N)    \
     X(KID_ATTN_ROWS) X(KID_ATTN_W64) X(KID_ATTN_W128) X(KID_ATTN_DQ_W64) X(KID_ATTN_DQ_W128) X(KID_ATTN_DK_W64) X(KID_ATTN_DK_W128)    \
     X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128) X(KID_ATTN_T64) X(KID_ATTN_T128) X(KID_ATTN_DQ_T64) X(KID_ATTN_DQ_T128)    \
-    X(KID_ATTN_DK_T64) X(KID_ATTN_DK_T128) X(KID_ATTN_DV_T64) X(KID_ATTN_DV_T128)
+    X(KID_ATTN_DK_T64) X(KID_ATTN_DK_T128) X(KID_ATTN_DV_T64) X(KID_ATTN_DV_T128)    \
+    X(KID_ATTN_DKV_T64) X(KID_ROPE_BOTH_4) X(KID_ROPE_BOTH_8) X(KID_ROPE_BOTH_N)
 
 // A batch-norm epilogue is written into a task's argument block by type (C3Args or PwArgs, whose `ep` fields sit at
 // different offsets): the predicates that name the type must agree with the type the kernel takes.

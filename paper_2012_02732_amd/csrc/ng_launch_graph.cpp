@@ -16,6 +16,12 @@
 
 namespace ng {
 
+// Two attention operators' parameters agree.
+static bool same_attention(const ng_op_params& a, const ng_op_params& b) {
+    return a.heads == b.heads && a.kv_heads == b.kv_heads && a.rot == b.rot && a.interleaved == b.interleaved && a.eps == b.eps && a.factor == b.factor &&
+           a.scale == b.scale;
+}
+
 // Which tasks have no launch of their own in modes 0-3:
 //   * a batch-norm / ReLU whose only input is a convolution result is applied by that
 //     convolution's kernel (fused_into[v] = the convolution);
@@ -25,6 +31,8 @@ namespace ng {
 //     (`one_stream`: of the whole submission order; fused_into[v] = that update). A later launch is always in order
 //     for an update: it already comes after every reader of its weights, and it keeps its place in the stream, so
 //     the last one's launch comes after everything the earlier ones waited for;
+//   * the input gradient and gamma's gradient of a norm and rotation of heads, and dk and dv of an attention with heads of up to 64
+//     channels, likewise share a launch with the work that both need done once;
 //   * the input gradient and the parameter gradients of a batch-norm (same dy, same x) are computed by one launch, at
 //     the place of whichever of the two tasks comes first on their stream (fused_into[the later one] = the earlier
 //     one). Both are ready when the first one is (same inputs), each tensor has its buffer to itself, and the later
@@ -94,6 +102,24 @@ void decide_launch_fusion(const ng_graph* g, const std::vector<Task>& tasks, boo
             for (int v = 0; v < n; ++v) taken = taken || fused_into[v] == w || fused_into[v] == d;
             if (!ready || taken) continue;
             fused_into[late] = early;
+            break;
+        }
+    }
+    // the gradients of a norm and rotation, and dk and dv of an attention, read the same tensors: one launch, at the place of whichever
+    // comes first (everything they read comes before both)
+    for (int d = 0; d < n; ++d) {
+        const Node& nd = g->nodes[d];
+        if ((nd.op != NG_OP_HEAD_ROPE_DGRAD && nd.op != NG_OP_ATTENTION_DK) || !tasks[d].fn || fused_into[d] >= 0) continue;
+        for (int w = 0; w < n; ++w) {
+            const Node& nw = g->nodes[w];
+            if (nw.op != (nd.op == NG_OP_HEAD_ROPE_DGRAD ? NG_OP_HEAD_ROPE_WGRAD : NG_OP_ATTENTION_DV) || !tasks[w].fn || fused_into[w] >= 0 ||
+                nw.preds != nd.preds || nw.weights != nd.weights || !same_attention(nd.p, nw.p) || !can_pair(tasks[d], tasks[w]))
+                continue;
+            if (!one_stream && sc.stream_of[w] != sc.stream_of[d]) continue;
+            bool taken = false;
+            for (int v = 0; v < n; ++v) taken = taken || fused_into[v] == w || fused_into[v] == d;
+            if (taken) continue;
+            if (pos[d] < pos[w]) fused_into[w] = d; else fused_into[d] = w;
             break;
         }
     }

@@ -226,6 +226,10 @@ static int pair_kid(const Task& first, const Task& second) {
         return dw_wgrad_by_quads(*reinterpret_cast<const DwGradArgs*>(second.args)) ? KID_PAIR_DW_LDS : KID_NONE;
     if (kid_first == KID_PW_PX_DGRAD && kid_second == KID_PW_WGRAD_PX) return KID_PAIR_PW16;
     if (kid_first == KID_PW_PX_DGRAD && kid_second == KID_PW_WGRAD_PX2) return KID_PAIR_PW32;
+    if (kid_first == KID_ATTN_DK_T64 && kid_second == KID_ATTN_DV_T64) return KID_ATTN_DKV_T64;
+    if (kid_first == KID_ROPE_DX_4 && kid_second == KID_ROPE_DG_4) return KID_ROPE_BOTH_4;
+    if (kid_first == KID_ROPE_DX_8 && kid_second == KID_ROPE_DG_8) return KID_ROPE_BOTH_8;
+    if (kid_first == KID_ROPE_DX_N && kid_second == KID_ROPE_DG_N) return KID_ROPE_BOTH_N;
     return KID_NONE;
 }
 bool can_pair(const Task& first, const Task& second) { return pair_kid(first, second) != KID_NONE; }
@@ -263,12 +267,30 @@ static void set_pw_backward(const Task& dgrad, const Task& wgrad, Task& t) {
     t.block[0] = kBlock;
     set_kernel<KID>(t, p, pw_backward_tiles(p.na, p.nb, p.b.splits));
 }
+// Both gradients of norm and rotation: the walk of the weight gradient, whose workgroups leave rows of sums, with dx written on the way.
+template <int KID>
+static void set_rope_backward(const Task& dgrad, const Task& wgrad, Task& t) {
+    RopeArgs a, d;
+    std::memcpy(&a, wgrad.args, sizeof a);
+    std::memcpy(&d, dgrad.args, sizeof d);
+    a.y = d.y;
+    t = Task();
+    t.block[0] = kBlock;
+    set_kernel<KID>(t, a, wgrad.ntiles);
+}
 void make_pair_task(const Task& first, const Task& second, Task& t) {
     switch (pair_kid(first, second)) {
         case KID_PAIR_DW: set_pair<KID_PAIR_DW>(first, second, t); break;
         case KID_PAIR_DW_LDS: set_pair<KID_PAIR_DW_LDS>(first, second, t); break;
         case KID_PAIR_PW16: set_pw_backward<KID_PAIR_PW16>(first, second, t); break;
         case KID_PAIR_PW32: set_pw_backward<KID_PAIR_PW32>(first, second, t); break;
+        case KID_ATTN_DKV_T64:                                  // the same workgroups for both
+            set_pair<KID_ATTN_DKV_T64>(first, second, t);
+            t.ntiles = first.ntiles, t.grid[0] = (unsigned)first.ntiles;
+            break;
+        case KID_ROPE_BOTH_4: set_rope_backward<KID_ROPE_BOTH_4>(first, second, t); break;
+        case KID_ROPE_BOTH_8: set_rope_backward<KID_ROPE_BOTH_8>(first, second, t); break;
+        case KID_ROPE_BOTH_N: set_rope_backward<KID_ROPE_BOTH_N>(first, second, t); break;
         default: t = first; break;
     }
 }
@@ -641,11 +663,19 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     } else if (nd.op != NG_OP_ATTENTION && columns > 32) {
         p.kid = nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_T64 : KID_ATTN_DQ_T128) : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_T64 : KID_ATTN_DK_T128)
               : (narrow ? KID_ATTN_DV_T64 : KID_ATTN_DV_T128);
-        per_block = kAttentionColumns, other = kGradientBlock, few = 2, workgroups = narrow ? 512 : 256;
+        per_block = kAttentionColumns, other = kGradientBlock, few = 2, workgroups = 512;
     }
     p.col_blocks = (int)ceil_div(columns, per_block);
     const long groups = q.n * nd.p.kv_heads * p.col_blocks, blocks = by_keys ? group * ceil_div(Tq, other) : ceil_div(Tk, other);
-    const long want = std::max<long>(1, std::min<long>(ceil_div(blocks, few), ceil_div(workgroups, groups)));
+    long want = std::max<long>(1, std::min<long>(ceil_div(blocks, few), ceil_div(workgroups, groups)));
+    if (per_block == kAttentionColumns) {
+        // A block costs a workgroup 2 (64 channels) to 4 us, a split what the workgroup that joins them reads, 0.4 and 1 us: the sum is
+        // smallest near these many. dq of 64 queries of four heads of 64 channels, 4096 keys: 8 splits 42, 16 29, 32 25 us; 16 heads of 128, 100
+        // queries, 4000 keys: 8 82, 16 59, 32 80; without splits 255 and 498.
+        want = std::min<long>({want, kMaxSplits, std::max<long>(1, std::lround(std::sqrt((narrow ? 5.0 : 3.0) * (double)blocks)))});
+        few = 1;
+    }
+    want = knob_int("NG_ATTN_SPLITS", 1, 32, want);
     p.per_split = (int)(ceil_div(ceil_div(blocks, want), few) * few);
     p.splits = (int)ceil_div(blocks, p.per_split);
     p.tiles = groups * p.splits;
