@@ -100,7 +100,8 @@ enum {
     NG_OP_HEAD_ROPE_DGRAD = 26, /* preds {dy, x, positions}, same weights and parameters -> dx */
     NG_OP_HEAD_ROPE_WGRAD = 27, /* preds {dy, x, positions}, weights {frequencies, gamma} -> dgamma as [1][d][1][1] */
     NG_OP_ATTENTION = 28,     /* preds {q, k, v} or {q, k, v, lengths}, no weights. q has c = heads d channels and Tq tokens, k and v
-                                 have kv_heads d channels and Tk tokens, of another sequence or of the same one; d <= 128; query
+                                 have kv_heads d channels and Tk tokens, of another sequence or of the same one; d <= 128, Tq and Tk
+                                 <= 2^22; query
                                  head i reads key head i / (heads / kv_heads), kv_heads a divisor of heads. lengths [n][1][1][1]:
                                  image b has the keys j < lengths[b] (not a number: none), whatever lies behind them in k and v;
                                  y[i] = sum_j p[i][j] v[j], p[i][.] = softmax over these keys of scale <q[i], k[j]>; a query

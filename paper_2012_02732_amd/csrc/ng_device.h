@@ -88,7 +88,7 @@ constexpr bool is_c3_patch(int kid) { return kid >= KID_C3_P64 && kid <= KID_C3_
 constexpr int c3_patches(int kid) { return kid == KID_C3_SK ? 4 : kid == KID_C3_P64 || kid == KID_C3_P96 || kid == KID_C3_Q32 ? 2 : 1; }
 constexpr int c3_patch_pixels(int kid) { return kid == KID_C3_SK ? 160 : kid == KID_C3_Q64 ? 384 : kid == KID_C3_R32 || kid == KID_C3_R128 ? 640 : 256; }
 // wavefronts per SIMD that the registers of a stand-alone kernel must leave room for: the compiler takes more than half of them for 96 rows
-constexpr int min_waves(int kid) { return (is_c3_patch(kid) && kid != KID_C3_SK) || is_attention_tile_kernel(kid) ? 2 : 1; }
+constexpr int min_waves(int kid) { return (is_c3_patch(kid) && kid != KID_C3_SK) || is_attention_tile_kernel(kid) || kid == KID_ATTN_W128 ? 2 : 1; }
 constexpr bool is_pw_columns(int kid) { return (kid >= KID_PW_V1 && kid <= KID_PW_S4) || kid == KID_PW_P32 || kid == KID_PW_P64; }   // tiles = row tiles x column blocks
 constexpr bool is_pw_patch(int kid) { return kid == KID_PW_P32 || kid == KID_PW_P64; }
 // windowed kernels for large tensors (batches): not in the lean build, but in the full and the train build

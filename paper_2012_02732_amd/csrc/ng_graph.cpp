@@ -21,6 +21,7 @@ bool in_set(int v, int a, int b) { return v == a || v == b; }
 
 // Attention operators address one head of one image (attention: the heads of q that share a key head) by 32-bit byte offsets.
 constexpr int64_t kMaxSliceElems = (int64_t)1 << 29;
+constexpr int64_t kMaxAttentionTokens = (int64_t)1 << 22;    // 128 channels of them are within 2^31 bytes, whatever the head has
 constexpr int64_t kMaxAttentionTiles = (int64_t)1 << 22;     // blocks of 16 columns; a launch has fewer than 2^24 workgroups
 
 // Output shape of an operator, or an error text. Mirrors the operator table in the header.
@@ -254,6 +255,7 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
             const int64_t d = q.c / p.heads;
             if (!(k == v) || k.n != q.n || k.c != d * p.kv_heads) return "attention: k and v must be [n][kv_heads * channels of a head] x tokens for q [n][heads * channels of a head]";
             const int64_t Tq = q.h * q.w, Tk = k.h * k.w;
+            if (Tq > kMaxAttentionTokens || Tk > kMaxAttentionTokens) return "attention: more than 2^22 tokens";
             if (Tq * d * (p.heads / p.kv_heads) > kMaxSliceElems || Tk * d > kMaxSliceElems)
                 return "attention: a head of k, or the heads of q that read it, have more than 2^29 values";
             if (q.n * p.kv_heads * ((std::max(Tq * (p.heads / p.kv_heads), Tk) + 15) / 16) > kMaxAttentionTiles) return "attention: too many heads and tokens for one launch";

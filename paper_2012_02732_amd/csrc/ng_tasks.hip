@@ -674,6 +674,8 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
         // queries, 4000 keys: 8 82, 16 59, 32 80; without splits 255 and 498.
         want = std::min<long>({want, kMaxSplits, std::max<long>(1, std::lround(std::sqrt((narrow ? 5.0 : 3.0) * (double)blocks)))});
         few = 1;
+    } else {
+        want = std::min<long>({want, kMaxWaveSplits, std::max<long>(1, std::lround(std::sqrt(6.0 * (double)blocks)))});
     }
     want = knob_int("NG_ATTN_SPLITS", 1, 32, want);
     p.per_split = (int)(ceil_div(ceil_div(blocks, want), few) * few);

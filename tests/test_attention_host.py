@@ -90,8 +90,11 @@ def test_attention_shapes_and_refusals():
 
 def test_extents_beyond_32_bit_offsets_and_launches_are_refused():
     long = 1 << 24
-    g = G(q=(1, 128, 1, 4), k=(1, 64, 1, long), ks=(1, 32, 1, long), qs=(1, 32, 1, 4), x=(1, 64, 1, long), pos=(1, 1, 1, long), tiny=(1 << 23, 1, 1, 1))
-    g.refused(B.NG_ESHAPE, "2^29", B.NG_OP_ATTENTION, ["q", "k", "k"], heads=2, kv_heads=1)
+    most = 1 << 22
+    g = G(q=(1, 256, 1, 4), k=(1, 128, 1, most), ks=(1, 32, 1, most), qs=(1, 32, 1, 4), kl=(1, 32, 1, most + 1), long=(1, 2048, 1, 1 << 19), k4=(1, 64, 1, 4), x=(1, 64, 1, long), pos=(1, 1, 1, long), tiny=(1 << 23, 1, 1, 1))
+    assert g.add(B.NG_OP_ATTENTION, ["q", "k", "k"], heads=2, kv_heads=1) > 0
+    g.refused(B.NG_ESHAPE, "2^22", B.NG_OP_ATTENTION, ["qs", "kl", "kl"], heads=1, kv_heads=1)
+    g.refused(B.NG_ESHAPE, "2^29", B.NG_OP_ATTENTION, ["long", "k4", "k4"], heads=32, kv_heads=1)      # the heads of q that read one of k
     assert g.add(B.NG_OP_ATTENTION, ["qs", "ks", "ks"], heads=1, kv_heads=1) > 0
     g.refused(B.NG_ESHAPE, "2^29", B.NG_OP_HEAD_ROPE, ["x", "pos"], 1, heads=1, rot=2)
     g.refused(B.NG_ESHAPE, "too many", B.NG_OP_ATTENTION, ["tiny", "tiny", "tiny"], heads=1, kv_heads=1)
