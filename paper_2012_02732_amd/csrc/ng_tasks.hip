@@ -657,10 +657,18 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
           : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_W64 : KID_ATTN_DK_W128) : (narrow ? KID_ATTN_DV_W64 : KID_ATTN_DV_W128);
     const long columns = by_keys ? Tk : group * Tq;
     long per_block = 16, other = 64, few = 4, workgroups = 1024;   // columns of a workgroup, the other side's in a block, blocks a split has at least
-    if (nd.op == NG_OP_ATTENTION && columns > 32) {
+    // Straight from memory with 16 columns a wavefront, or 128 columns a workgroup through LDS. The former where there are few
+    // columns, and where the whole task is a wavefront and block for each of at most 768 wavefronts, three on a compute unit, which
+    // then takes as long as one block. Forward, us straight / through LDS: 256 x 256 with one head 7.0 / 13.4 (64 wavefronts), 128 x 77
+    // with 16 heads 7.4 / 9.4 (256), 48 x 512 with 32 heads of 128 17.5 / 23.4 (768), 64 x 64 with 256 heads 13.1 / 6.5 (1024), 256 x 77 with
+    // 64 heads 17.5 / 8.9 (2048); dq 12.4 / 13.3, 11.8 / 13.6, 24.4 / 29.5, 23.5 / 12.3, 19.6 / 12.6. dk and dv share a launch through LDS with up
+    // to 64 channels; with more, 128 x 128 with four heads 21 + 15 / 24 + 18 (64), 48 x 512 with 32 heads 49 + 35 / 18 + 13 (1024).
+    const long wavefronts = q.n * nd.p.kv_heads * ceil_div(columns, 16) * (by_keys ? group * ceil_div(Tq, 64) : ceil_div(Tk, 64));
+    const bool tiles = columns > 32 && (wavefronts > 768 || (by_keys && narrow));
+    if (nd.op == NG_OP_ATTENTION && tiles) {
         p.kid = narrow ? KID_ATTN_T64 : KID_ATTN_T128;
         per_block = kAttentionColumns, other = narrow ? attention_block<64>() : attention_block<128>(), few = 2, workgroups = 512;
-    } else if (nd.op != NG_OP_ATTENTION && columns > 32) {
+    } else if (tiles) {
         p.kid = nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_T64 : KID_ATTN_DQ_T128) : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_T64 : KID_ATTN_DK_T128)
               : (narrow ? KID_ATTN_DV_T64 : KID_ATTN_DV_T128);
         per_block = kAttentionColumns, other = kGradientBlock, few = 2, workgroups = 512;

@@ -318,3 +318,12 @@ def test_replays_follow_their_inputs_and_each_other():
     finally:
         for g, r in graphs:
             r.close()
+
+
+@pytest.mark.parametrize("case", [(1, 1, 1, 64, 256, 256, None), (2, 8, 8, 64, 128, 77, "ragged"), (4, 8, 8, 128, 48, 512, "ragged"), (16, 16, 16, 64, 64, 64, "odd"),
+                                  (8, 8, 8, 40, 256, 77, None), (4, 4, 4, 128, 128, 128, None)], ids=str)
+def test_attention_on_both_sides_of_the_choice_of_kernels(case):
+    n, heads, kv_heads, d, tq, tk, kind = case
+    q, k, v, dy, ln = attention_inputs(tq + tk, n, heads, kv_heads, d, tq, tk, kind)
+    g = attention_graph(q, k, v, dy, ln, heads, kv_heads, d ** -0.5)
+    check_attention(run(g)[B.NG_MODE_GRAPH_SINGLE], q, k, v, dy, ln, heads, kv_heads, d ** -0.5, case)
