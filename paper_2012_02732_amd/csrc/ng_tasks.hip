@@ -724,14 +724,15 @@ RopePlan rope_plan(const ng_graph* g, int v) {
         p.kid = (d <= 128 ? KID_ROPE_4 : KID_ROPE_8) + 3 * which;
         p.blocks = (int)ceil_div(T, 64);
         p.items = (int)(x.n * p.blocks);
-        p.heads_per_tile = (int)std::max<long>(1, std::min<long>(H, (long)p.items * H / (wgrad ? 512 : 1024)));
+        // (wgrad, and with it both gradients in one launch, has two workgroups on a compute unit: 700 blocks of heads of 64 channels by
+        // themselves take two turns and 22 us, two of a workgroup 17)
+        p.heads_per_tile = (int)std::max<long>(1, std::min<long>(H, wgrad ? ceil_div((long)p.items * H, 512) : (long)p.items * H / 1024));
         p.per_tile = (int)ceil_div(p.items, most);
         p.tiles = ceil_div(p.items, p.per_tile) * ceil_div(H, p.heads_per_tile);
     }
     if (wgrad) {
-        const long groups = ceil_div(p.tiles, kGammaGroup);
-        p.ws_floats = (size_t)round64((p.tiles + groups) * d);
-        p.cnt_words = (size_t)round64(1 + groups);
+        p.ws_floats = (size_t)round64(p.tiles * d);
+        p.cnt_words = (size_t)round64(1 + ceil_div(p.tiles, kGammaGroup));
     }
     return p;
 }
