@@ -107,8 +107,8 @@ enum {
                                  y[i] = sum_j p[i][j] v[j], p[i][.] = softmax over these keys of scale <q[i], k[j]>; a query
                                  without any key: 0. q, and the keys and values that count, have to be finite */
     NG_OP_ATTENTION_ROWS = 29, /* preds {dy, y}, y an NG_OP_ATTENTION node, heads as there -> [n][3 heads] x tokens of y: for each query
-                                 <dy, y> of its head, the largest score (times log2 e) of its keys, and one over the sum of their
-                                 2^(score - largest); 0 and 0 without any key. What the three gradients need of every query */
+                                 <dy, y> of its head, a reference near the largest score (times log2 e) of its keys, and one over
+                                 the sum of their 2^(score log2 e - reference); 0 and 0 without any key. What the three gradients need of every query */
     NG_OP_ATTENTION_DQ = 30,  /* preds {dy, rows, q, k, v[, lengths]} of one attention, heads, kv_heads and scale as there; rows: its */
     NG_OP_ATTENTION_DK = 31,  /* NG_OP_ATTENTION_ROWS node -> dq, dk (shapes of q, k; 0 for keys that do not count) */
     NG_OP_ATTENTION_DV = 32   /* -> dv */
@@ -129,8 +129,8 @@ typedef struct ng_op_params {
     int32_t kv_heads;  /* ATTENTION, _DQ, _DK, _DV: heads of k and v */
     int32_t rot;       /* HEAD_ROPE*: channels of a head that are rotated */
     int32_t interleaved; /* HEAD_ROPE*: which channels are a pair */
-    float factor;      /* HEAD_ROPE*: on the rotated channels (1: a rotation; scaled long contexts may want another) */
-    float scale;       /* ATTENTION, _DQ, _DK, _DV: on the scores */
+    float factor;      /* HEAD_ROPE*: on the rotated channels (1: a rotation; scaled long contexts may want another), not 0 */
+    float scale;       /* ATTENTION, _DQ, _DK, _DV: on the scores, not 0 */
 } ng_op_params;
 
 typedef struct ng_graph ng_graph; /* opaque */

@@ -231,7 +231,7 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
             if (p.rot < 2 || p.rot % 2 != 0 || p.rot > d) return "head_rope: rot must be even, 2 .. channels of a head";
             if (!in_set(p.interleaved, 0, 1)) return "head_rope: interleaved in {0,1}";
             if (!(p.eps >= 0.f) || !std::isfinite(p.eps)) return "head_rope: eps must be >= 0 and finite";
-            if (!std::isfinite(p.factor)) return "head_rope: factor must be finite";
+            if (!std::isfinite(p.factor) || p.factor == 0.f) return "head_rope: factor must be finite and not 0";
             code = NG_ESHAPE;
             if (backward && !(in(0) == x)) return "head_rope backward: dy and x differ in shape";
             if ((pos.n != 1 && pos.n != x.n) || pos.c != 1 || pos.h != x.h || pos.w != x.w)
@@ -249,7 +249,7 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
                 return first ? "attention backward takes dy, rows, q, k, v and, if the attention has them, lengths" : "attention takes q, k, v and, if wanted, lengths";
             const Shape &q = in(first), &k = in(first + 1), &v = in(first + 2);
             if (p.heads <= 0 || p.kv_heads <= 0 || p.heads % p.kv_heads != 0) return "attention: kv_heads must be positive and divide heads";
-            if (!std::isfinite(p.scale)) return "attention: scale must be finite";
+            if (!std::isfinite(p.scale) || p.scale == 0.f) return "attention: scale must be finite and not 0";
             code = NG_ESHAPE;
             if (q.c % p.heads != 0 || q.c / p.heads > kAttentionMaxHead) return "attention: heads must divide the channels of q, at most 128 channels a head";
             const int64_t d = q.c / p.heads;

@@ -179,6 +179,7 @@ void compute_schedule(int n, const std::vector<std::pair<int, int>>& edges, Sche
 int build_task(ng_graph* g, int v, char* arena, float* packed, Task& t);
 size_t packed_floats(const ng_graph* g, int v);
 int pack_constants(ng_graph* g, int v, float* packed, void* stream);
+bool has_arrival_counters(int op);           // pack_constants sets a node's arrival counters back, and does nothing else
 template <int BUILD> const void* resident_build_handle();   // defined in ng_resident.hip, one specialisation per object
 const void* resident_kernel_handle(int build);
 const void* empty_kernel_handle();

@@ -549,6 +549,10 @@ int launch_resident(ng_graph* g) {
         NG_HIP(hipStreamSynchronize(origin));
         NG_HIP(hipMemsetAsync(rt.plan.done, 0, (10 * rt.done_words + 18) * sizeof(unsigned), origin));   // on the stream of the launch below
         NG_HIP(hipMemsetAsync(rt.plan.error_dev, 0, sizeof(int), origin));
+        // a replay that gave up may have left workgroups of a task uncounted that the last one to arrive waits for
+        for (int v = 0; v < (int)g->nodes.size(); ++v)
+            if (has_arrival_counters(g->nodes[v].op) && g->packed_of[v])
+                if (int rc = pack_constants(g, v, g->packed_of[v], origin)) return rc;
         *rt.h_error = 0;
         rt.epoch = 0;
         rt.counters_dirty = false;
@@ -860,10 +864,12 @@ int ng_replay(ng_graph* g) {
                                           "(%d replays compared); choose another replay mode", g->graph_multi_checked);
             NG_HIP(hipGraphLaunch(rt.exec[0], rt.streams[0]));
             return NG_OK;
-        case NG_MODE_GRAPH_SINGLE:
-            if (g->single_launches.size() <= kDirectLaunches) return issue_all(g, false);
+        case NG_MODE_GRAPH_SINGLE: {
+            int dev = -1;                                       // a graph launch does not ask which device is current, a kernel launch does
+            if (g->single_launches.size() <= kDirectLaunches && hipGetDevice(&dev) == hipSuccess && dev == rt.device) return issue_all(g, false);
             NG_HIP(hipGraphLaunch(rt.exec[1], rt.streams[0]));
             return NG_OK;
+        }
         case NG_MODE_EAGER_SINGLE: return issue_all(g, false);
         case NG_MODE_EAGER_MULTI: return issue_all(g, true);
         default: return launch_resident(g);

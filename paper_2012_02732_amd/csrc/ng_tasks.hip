@@ -769,6 +769,10 @@ size_t packed_floats(const ng_graph* g, int v) {
     return choose_pw(g, v).packed;
 }
 
+bool has_arrival_counters(int op) {
+    return op == NG_OP_CONV1X1_WGRAD || op == NG_OP_CONV3X3_WGRAD || op == NG_OP_DWCONV_WGRAD || op == NG_OP_BN_ACT_WGRAD || is_attention_op(op) || is_rope_op(op);
+}
+
 // Fill node v's constant memory: one pass over the weights, at bind time.
 int pack_constants(ng_graph* g, int v, float* packed, void* stream) {
     const Node& nd = g->nodes[v];

@@ -40,7 +40,7 @@ def test_head_rope_shapes_and_refusals():
     assert tuple(B.ng_node_shape(g.g, g.add(dgrad, [y, "x", "pos"], 1))) == (2, 12, 3, 5)
     assert tuple(B.ng_node_shape(g.g, g.add(wgrad, [y, "x", "pos"], 2))) == (1, 6, 1, 1)
     for bad in (dict(heads=0), dict(heads=5), dict(heads=-2), dict(rot=0), dict(rot=3), dict(rot=8), dict(rot=-2), dict(interleaved=2),
-                dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(factor=float("nan")), dict(factor=float("inf"))):
+                dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(factor=float("nan")), dict(factor=float("inf")), dict(factor=0.0)):
         g.refused(B.NG_EINVAL, "head_rope", rope, ["x", "pos"], 2, **bad)
     g.refused(B.NG_EINVAL, "256", rope, ["wide", "pos4"], 1, heads=2)
     for n_weights in (0, 3):
@@ -72,7 +72,7 @@ def test_attention_shapes_and_refusals():
         g.refused(B.NG_EINVAL, "attention_rows node of dy", op, ["dy", y, "q", "k", "v"], **how)
         g.refused(B.NG_EINVAL, "takes dy, rows", op, ["dy", rows, "q", "k"], **how)
     for bad in (dict(heads=4, kv_heads=3), dict(heads=0, kv_heads=1), dict(heads=4, kv_heads=0), dict(heads=4, kv_heads=-2), dict(heads=4, kv_heads=2, scale=float("inf")),
-                dict(heads=4, kv_heads=2, scale=float("nan"))):
+                dict(heads=4, kv_heads=2, scale=float("nan")), dict(heads=4, kv_heads=2, scale=0.0)):
         g.refused(B.NG_EINVAL, "attention", att, ["q", "k", "v"], **bad)
     g.refused(B.NG_ESHAPE, "128", att, ["big", "big", "big"], heads=2, kv_heads=2)
     g.refused(B.NG_ESHAPE, "heads must divide", att, ["q", "k", "v"], heads=5, kv_heads=5)
@@ -101,30 +101,8 @@ def test_extents_beyond_32_bit_offsets_and_launches_are_refused():
     B.ng_destroy(g.g)
 
 
-def decoder(n=2, heads=4, kv_heads=2, d=8, tokens=6, states=9, seed=0):
-    """A block that attends to another sequence's states: projections, norm and rotation of the heads, attention, projection, sum."""
-    rng = np.random.default_rng(seed)
-    b = workloads.Builder("decoder_block")
-    x = b.input(n, 24, 1, tokens)
-    memory, at, at_memory, lengths = b.input(n, 20, 1, states), b.input(1, 1, 1, tokens), b.input(n, 1, 1, states), b.input(n, 1, 1, 1)
-    x = b.conv1x1(x, heads * d)
-    f = workloads.rope_frequencies(d)
-    q = b.head_rope(x, at, heads, f)
-    k = b.head_rope(b.conv1x1(memory, kv_heads * d), at_memory, kv_heads, f)
-    v = b.conv1x1(memory, kv_heads * d)
-    y = b.attention(q, k, v, heads, kv_heads, lengths)
-    y = b.add_n([b.conv1x1(y, heads * d), x])
-    s = b.head_rope(b.conv1x1(y, heads * d), at, heads, f[:2], norm=False, interleaved=True)      # attention of a sequence to itself
-    b.attention(s, s, b.conv1x1(y, heads * d), heads)
-    b.draw_weights(rng, "he", "random")
-    w = b.finish(rng)
-    w.inputs = {memory: rng.standard_normal((n, 20, 1, states)).astype(np.float32), at: np.arange(tokens, dtype=np.float32).reshape(1, 1, 1, -1) + 100,
-                at_memory: rng.integers(0, 50, (n, 1, 1, states)).astype(np.float32), lengths: np.array([states - 2] + [0] * (n - 1), np.float32).reshape(n, 1, 1, 1)}
-    return w
-
-
 def test_training_graph_of_a_block_with_attention():
-    w = decoder()
+    w = workloads.decoder_block()
     out = w.outputs[0]
     seed = np.random.default_rng(1).standard_normal(w.nodes[out].shape).astype(np.float32)
     tw = workloads.training_graph(w, 0.01, {out: seed})

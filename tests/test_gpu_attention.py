@@ -245,14 +245,13 @@ def test_zero_rows_and_eps():
 
 def _decoder_training(**sizes):
     import workloads
-    from test_attention_host import decoder
-    w = decoder(**sizes)
+    w = workloads.decoder_block(**sizes)
     out = w.outputs[0]
     seed = np.random.default_rng(1).standard_normal(w.nodes[out].shape).astype(np.float32)
     return w, out, seed, workloads.training_graph(w, 0.01, {out: seed})
 
 
-@pytest.mark.parametrize("sizes", [{}, dict(n=3, heads=8, kv_heads=2, d=64, tokens=150, states=211)], ids=["small", "larger"])
+@pytest.mark.parametrize("sizes", [{}, dict(batch=3, heads=8, kv_heads=2, d=64, tokens=150, states=211)], ids=["small", "larger"])
 def test_training_step_of_a_block_with_attention(sizes):
     """Forward pass, gradients and update of a decoder block as one graph, in every mode that has a plan for it: gradients against the
     oracle on the forward tensors that the GPU stored, updated weights against its update, and the weights as they were after capture."""
@@ -327,3 +326,67 @@ def test_attention_on_both_sides_of_the_choice_of_kernels(case):
     q, k, v, dy, ln = attention_inputs(tq + tk, n, heads, kv_heads, d, tq, tk, kind)
     g = attention_graph(q, k, v, dy, ln, heads, kv_heads, d ** -0.5)
     check_attention(run(g)[B.NG_MODE_GRAPH_SINGLE], q, k, v, dy, ln, heads, kv_heads, d ** -0.5, case)
+
+
+@pytest.mark.parametrize("dy_size,v_size", [(1e-20, 1e-11), (1e-33, 1.0), (1e-3, 1e-30)])
+def test_attention_gradients_of_small_products(dy_size, v_size):
+    """<dy, v> far below one, but a normal number: 2^-100 and less."""
+    q, k, v, dy, ln = attention_inputs(9, 2, 4, 2, 64, 200, 300, "ragged", dy_scale=dy_size)
+    v = np.where(np.isfinite(v), v * np.float32(v_size), v).astype(np.float32)
+    g = attention_graph(q, k, v, dy, ln, 4, 2, 0.125)
+    got = run(g)[B.NG_MODE_GRAPH_SINGLE]
+    ref = attention_reference(q, np.nan_to_num(k), np.where(np.isfinite(v), v, 0), dy, ln, 4, 2, 0.125)
+    for name in ("y", "dq", "dk", "dv"):                        # sums of a few hundred terms that cancel: as in check_attention, 400 u
+        assert norm_off(got[name], ref[name]) <= 400 * U, (name, norm_off(got[name], ref[name]))
+
+
+@pytest.mark.parametrize("how", ["reuse", "no_fusion", "device_scope"])
+def test_attention_under_other_plans(how):
+    """Buffers handed on, one launch for each task, every hand-over through device scope: the same results."""
+    q, k, v, dy, ln = attention_inputs(11, 3, 4, 2, 40, 50, 90, "ragged")
+    g = attention_graph(q, k, v, dy, ln, 4, 2, 0.2)
+    plain = run(g)[B.NG_MODE_GRAPH_SINGLE]
+    if how == "reuse":
+        r = GraphRunner(g.workload(), DEV)
+        B.ng_set_memory_reuse(r.g, 1)
+        try:
+            r.prepare(plan_trials=1)
+            for mode in (B.NG_MODE_GRAPH_SINGLE, B.NG_MODE_GRAPH_MULTI):
+                r.arena.fill_(0xFF)
+                for node, t in g.inputs.items():
+                    r.set_input(t, node)
+                r.replay(mode)
+                for name in plain:
+                    assert np.array_equal(r.output(g.names[name]), plain[name]), (mode, name)
+        finally:
+            r.close()
+        return
+    got = run(g, MODES, **(dict(launch_fusion=False) if how == "no_fusion" else dict(resident_device_scope=1)))
+    for mode, tensors in got.items():
+        for name in plain:
+            # dk and dv in one launch are cut like each of them alone: the same sums
+            assert np.array_equal(tensors[name], plain[name]), (how, mode, name)
+
+
+def test_replay_after_one_that_gave_up():
+    """A device-resident replay whose waits run out of spins leaves arrival counters where they were: the next one starts afresh."""
+    q, k, v, dy, ln = attention_inputs(12, 2, 2, 2, 100, 20, 300, None)      # sizes whose kernels are in the resident build
+    g = attention_graph(q, k, v, dy, ln, 2, 2, 0.25)
+    r = GraphRunner(g.workload(), DEV)
+    try:
+        r.prepare(plan_trials=1)
+        r.replay(B.NG_MODE_DEVICE_RESIDENT)
+        first = {name: r.output(g.names[name]) for name in ("y", "dq", "dk", "dv")}
+        B.ng_resident_config(r.g, 0, 0, 1, 0)                   # one poll: somebody gives up
+        r.replay(B.NG_MODE_DEVICE_RESIDENT)
+        try:
+            r.sync()
+        except B.NgError as e:
+            assert e.code == B.NG_EHIP
+        B.ng_resident_config(r.g, 0, 0, 0, 0)
+        for _ in range(3):
+            r.replay(B.NG_MODE_DEVICE_RESIDENT)
+            for name in first:
+                assert np.array_equal(r.output(g.names[name]), first[name]), name
+    finally:
+        r.close()

@@ -38,3 +38,4 @@ Conventions shared by every consumer (an interface, not an implementation):
 from .model import Builder, Node, Workload, OPS, ATTENTION_OPS, TRAIN_OPS, rope_frequencies  # noqa: F401
 from .configs import make, CONFIG_NAMES  # noqa: F401
 from .training import training_graph, nas_cell_cifar, TrainingWorkload  # noqa: F401
+from .attention import decoder_block  # noqa: F401
