@@ -541,6 +541,14 @@ int tune_resident(ng_graph* g) {
     return rc;
 }
 
+// A replay that gave up may have left workgroups of a task uncounted: the counts of those that whoever is last adds up start over.
+int clear_arrival_counters(ng_graph* g) {
+    for (int v = 0; v < (int)g->nodes.size(); ++v)
+        if (has_arrival_counters(g->nodes[v].op) && g->packed_of[v])
+            if (int rc = pack_constants(g, v, g->packed_of[v], g->rt->streams[0])) return rc;
+    return NG_OK;
+}
+
 int launch_resident(ng_graph* g) {
     Runtime& rt = *g->rt;
     if (!rt.d_records) return g->fail(NG_ESTATE, "device-resident replay: this graph has no plan (an attention operator next to a kernel for large problems or a graph that trains)");
@@ -549,10 +557,7 @@ int launch_resident(ng_graph* g) {
         NG_HIP(hipStreamSynchronize(origin));
         NG_HIP(hipMemsetAsync(rt.plan.done, 0, (10 * rt.done_words + 18) * sizeof(unsigned), origin));   // on the stream of the launch below
         NG_HIP(hipMemsetAsync(rt.plan.error_dev, 0, sizeof(int), origin));
-        // a replay that gave up may have left workgroups of a task uncounted that the last one to arrive waits for
-        for (int v = 0; v < (int)g->nodes.size(); ++v)
-            if (has_arrival_counters(g->nodes[v].op) && g->packed_of[v])
-                if (int rc = pack_constants(g, v, g->packed_of[v], origin)) return rc;
+        if (int rc = clear_arrival_counters(g)) return rc;
         *rt.h_error = 0;
         rt.epoch = 0;
         rt.counters_dirty = false;
@@ -926,6 +931,8 @@ int ng_replay_static(ng_graph* g) {
     plan.spin_limit = g->resident_spin_limit;
     hipStream_t origin = rt.streams[0];
     if (*rt.h_error != 0) *rt.h_error = 0;                     // left by a replay that gave up (calls do not overlap, so it has ended)
+    if (rt.counters_dirty)
+        if (int rc = clear_arrival_counters(g)) return rc;
     const unsigned blocks = (unsigned)std::min<size_t>((need + 255) / 256, 1024);
     zero_words_kernel<<<dim3(blocks), dim3(256), 0, origin>>>(base, need);
     NG_HIP(hipGetLastError());

@@ -773,6 +773,17 @@ bool has_arrival_counters(int op) {
     return op == NG_OP_CONV1X1_WGRAD || op == NG_OP_CONV3X3_WGRAD || op == NG_OP_DWCONV_WGRAD || op == NG_OP_BN_ACT_WGRAD || is_attention_op(op) || is_rope_op(op);
 }
 
+namespace {
+__global__ __launch_bounds__(kBlock) void clear_words_kernel(float* p, size_t words) {
+    for (size_t i = (size_t)blockIdx.x * kBlock + threadIdx.x; i < words; i += (size_t)gridDim.x * kBlock) p[i] = 0.f;
+}
+// (a kernel: ng_replay_static, which records no memset, may have to do it)
+hipError_t clear_words(float* p, size_t words, void* stream) {
+    clear_words_kernel<<<dim3((unsigned)std::min<size_t>((words + kBlock - 1) / kBlock, 1024)), dim3(kBlock), 0, static_cast<hipStream_t>(stream)>>>(p, words);
+    return hipGetLastError();
+}
+}  // namespace
+
 // Fill node v's constant memory: one pass over the weights, at bind time.
 int pack_constants(ng_graph* g, int v, float* packed, void* stream) {
     const Node& nd = g->nodes[v];
@@ -781,14 +792,14 @@ int pack_constants(ng_graph* g, int v, float* packed, void* stream) {
         const AttentionPlan p = attention_plan(g, v);
         const RopePlan r = rope_plan(g, v);
         if (p.cnt_words + r.cnt_words == 0) return NG_OK;
-        const hipError_t e = hipMemsetAsync(packed + p.ws_floats + r.ws_floats, 0, (p.cnt_words + r.cnt_words) * sizeof(float), static_cast<hipStream_t>(stream));
+        const hipError_t e = clear_words(packed + p.ws_floats + r.ws_floats, p.cnt_words + r.cnt_words, stream);
         if (e != hipSuccess) return g->fail(NG_EHIP, "clearing arrival counters of an attention operator: %s", hipGetErrorString(e));
         return NG_OK;
     }
     if (wgrad_dims(g, v, &wm, &wn, &wk)) {                     // the arrival counters start at zero
         const WgradPlan p = wgrad_plan(g, v);
         if (p.cnt_words == 0) return NG_OK;
-        const hipError_t e = hipMemsetAsync(packed + p.ws_floats, 0, p.cnt_words * sizeof(float), static_cast<hipStream_t>(stream));
+        const hipError_t e = clear_words(packed + p.ws_floats, p.cnt_words, stream);
         if (e != hipSuccess) return g->fail(NG_EHIP, "clearing split-K counters: %s", hipGetErrorString(e));
         return NG_OK;
     }
@@ -796,7 +807,7 @@ int pack_constants(ng_graph* g, int v, float* packed, void* stream) {
         const size_t floats = packed_floats(g, v);
         if (floats == 0) return NG_OK;
         const size_t cnt = (size_t)((g->nodes[nd.preds[1]].out.c + 63) & ~63L);
-        const hipError_t e = hipMemsetAsync(packed + floats - cnt, 0, cnt * sizeof(float), static_cast<hipStream_t>(stream));
+        const hipError_t e = clear_words(packed + floats - cnt, cnt, stream);
         if (e != hipSuccess) return g->fail(NG_EHIP, "clearing depthwise wgrad counters: %s", hipGetErrorString(e));
         return NG_OK;
     }

@@ -384,8 +384,8 @@ def test_replay_after_one_that_gave_up():
         except B.NgError as e:
             assert e.code == B.NG_EHIP
         B.ng_resident_config(r.g, 0, 0, 0, 0)
-        for _ in range(3):
-            r.replay(B.NG_MODE_DEVICE_RESIDENT)
+        for again in (B.ng_replay_static, lambda _: r.replay(B.NG_MODE_DEVICE_RESIDENT), lambda _: r.replay(B.NG_MODE_GRAPH_SINGLE)):
+            again(r.g)
             for name in first:
                 assert np.array_equal(r.output(g.names[name]), first[name]), name
     finally:
