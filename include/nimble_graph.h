@@ -105,7 +105,10 @@ enum {
                                  head i reads key head i / (heads / kv_heads), kv_heads a divisor of heads. lengths [n][1][1][1]:
                                  image b has the keys j < lengths[b] (not a number: none), whatever lies behind them in k and v;
                                  y[i] = sum_j p[i][j] v[j], p[i][.] = softmax over these keys of scale <q[i], k[j]>; a query
-                                 without any key: 0. q, and the keys and values that count, have to be finite */
+                                 without any key: 0. q, and the keys and values that count, have to be finite, scale log2 e too.
+                                 Sums in fp32. With many columns the factors of a product are two half-precision parts in a unit of
+                                 the largest magnitude of a query, of a key head's keys, of its values (gradients: also of dy): 2^-13 of it
+                                 and more has all its bits, down to 2^-37 fewer and fewer, less is 0 */
     NG_OP_ATTENTION_ROWS = 29, /* preds {dy, y}, y an NG_OP_ATTENTION node, heads as there -> [n][3 heads] x tokens of y: for each query
                                  <dy, y> of its head, a reference near the largest score (times log2 e) of its keys, and one over
                                  the sum of their 2^(score log2 e - reference); 0 and 0 without any key. What the three gradients need of every query */
@@ -324,7 +327,12 @@ enum {
                                    inside the tiles of the task that produces its operand, and a concat whose
                                    inputs were produced in place runs nothing (ng_resident_fusion reports which);
                                    every node's tensor is written all the same and equals the other modes' bit
-                                   for bit. The plan passes a self-check at ng_capture or the capture fails. */
+                                   for bit. The plan passes a self-check at ng_capture or the capture fails.
+                                   A graph with attention operators has a plan if its tasks are small ones: no
+                                   attention over many queries (more than 768 pairs of 16 columns and 64 keys, where
+                                   32 columns are exceeded), no kernel for large images, no gradients of convolutions
+                                   and batch-norms. Without a plan the mode is no candidate of NG_MODE_AUTO, and this mode,
+                                   ng_replay_static and ng_resident_dry_plan return NG_ESTATE. */
     NG_MODE_AUTO = 5          /* the default: whichever of modes 0, 1 and 4 was fastest in a short trial at ng_capture (an
                                    ahead-of-time choice like the rest of the schedule: DAGs of many tiny tasks
                                    gain most from mode 4, plain chains and large tasks from a HIP graph) */

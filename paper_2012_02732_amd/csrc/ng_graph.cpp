@@ -249,7 +249,7 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
                 return first ? "attention backward takes dy, rows, q, k, v and, if the attention has them, lengths" : "attention takes q, k, v and, if wanted, lengths";
             const Shape &q = in(first), &k = in(first + 1), &v = in(first + 2);
             if (p.heads <= 0 || p.kv_heads <= 0 || p.heads % p.kv_heads != 0) return "attention: kv_heads must be positive and divide heads";
-            if (!std::isfinite(p.scale) || p.scale == 0.f) return "attention: scale must be finite and not 0";
+            if (!std::isfinite((float)(p.scale * 1.4426950408889634)) || p.scale == 0.f) return "attention: scale must be finite, also times log2 e, and not 0";
             code = NG_ESHAPE;
             if (q.c % p.heads != 0 || q.c / p.heads > kAttentionMaxHead) return "attention: heads must divide the channels of q, at most 128 channels a head";
             const int64_t d = q.c / p.heads;

@@ -206,6 +206,9 @@ void build_launch_graph(const ng_graph* g, const std::vector<Task>& tasks, const
 // ng_resident_plan.cpp: xcds = 0 lets the cost model choose among 1, 2, 4, 8.
 int plan_resident(const ng_graph* g, int n_wg, int xcds, const PlanKnobs& knobs, ResidentPlan& plan);
 bool resident_plan_is_consistent(const ng_graph* g, const ResidentPlan& plan);
+// Graphs with attention have a device-resident plan if the attention build has all their kernels; without attention: true.
+bool has_resident_plan(const std::vector<Task>& tasks);
+constexpr const char* kNoResidentPlan = "this graph has no device-resident plan: it has attention operators next to kernels for many columns, large images or training";
 // ng_runtime.hip
 void destroy_runtime(ng_graph* g);
 }  // namespace ng

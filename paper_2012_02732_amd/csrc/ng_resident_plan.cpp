@@ -679,6 +679,13 @@ int plan_resident(const ng_graph* g, int n_wg, int xcds, const PlanKnobs& knobs,
 
 namespace ng {
 
+bool has_resident_plan(const std::vector<Task>& tasks) {
+    bool attention = false, others = false;
+    for (const Task& t : tasks)
+        if (t.fn) attention = attention || is_attention_kernel(t.kid), others = others || !in_build(BUILD_ATTENTION, t.kid);
+    return !attention || !others;
+}
+
 // Self-check of a device-resident plan against the graph it was made for; true if it holds.
 bool resident_plan_is_consistent(const ng_graph* g, const ResidentPlan& plan) {
     // invariants: every tile of every task is covered exactly once, lists ascend in task id,
@@ -894,6 +901,7 @@ extern "C" int ng_resident_dry_plan_setting(ng_graph* g, int setting, int n_work
     static float fake_constants;
     for (int v = 0; v < (int)g->nodes.size() && rc == NG_OK; ++v) rc = build_task(g, v, fake_arena, &fake_constants, g->tasks[v]);
     ResidentPlan plan;
+    if (rc == NG_OK && !has_resident_plan(g->tasks)) rc = g->fail(NG_ESTATE, "ng_resident_dry_plan: %s", kNoResidentPlan);
     if (rc == NG_OK && plan_resident(g, n_workgroups, xcds, plan_setting(setting), plan) != NG_OK) rc = g->fail(NG_EINVAL, "too many E' parents");
     if (rc == NG_OK) {
         if (expected_us) *expected_us = plan.est_us;

@@ -324,8 +324,7 @@ int build_resident(ng_graph* g) {
     if (attention) {
         // the attention build takes graphs of small tasks; others are replayed through the HIP graphs only
         rt.resident_build = BUILD_ATTENTION;
-        for (const Task& t : g->tasks)
-            if (t.fn && !in_build(BUILD_ATTENTION, t.kid)) return NG_OK;
+        if (!has_resident_plan(g->tasks)) return NG_OK;
     }
     NG_HIP(hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, resident_kernel_handle(rt.resident_build), kGroup, 0));
     if (per_cu < 1 || cus < 8) return g->fail(NG_EHIP, "device-resident replay: kernel does not fit (%d per CU, %d CUs)", per_cu, cus);
@@ -551,7 +550,7 @@ int clear_arrival_counters(ng_graph* g) {
 
 int launch_resident(ng_graph* g) {
     Runtime& rt = *g->rt;
-    if (!rt.d_records) return g->fail(NG_ESTATE, "device-resident replay: this graph has no plan (an attention operator next to a kernel for large problems or a graph that trains)");
+    if (!rt.d_records) return g->fail(NG_ESTATE, "device-resident replay: %s", kNoResidentPlan);
     hipStream_t origin = rt.streams[0];
     if (rt.counters_dirty) {                                   // a timed-out replay left partial counts behind
         NG_HIP(hipStreamSynchronize(origin));
@@ -904,7 +903,7 @@ int ng_replay_static(ng_graph* g) {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_replay_static: call ng_capture first");
     Runtime& rt = *g->rt;
-    if (!rt.d_records) return g->fail(NG_ESTATE, "ng_replay_static: this graph has no device-resident plan");
+    if (!rt.d_records) return g->fail(NG_ESTATE, "ng_replay_static: %s", kNoResidentPlan);
     const size_t n = g->nodes.size();
     const size_t done_words = n * (size_t)rt.plan.done_stride;
     const size_t xcc_at = (10 * done_words + 1) & ~(size_t)1, error_at = xcc_at + 16, need = error_at + 2;
@@ -988,7 +987,8 @@ int ng_resident_plan_kept(const ng_graph* g, int* setting) {
 
 int ng_resident_trace(ng_graph* g, int enable, unsigned long long* ticks) {
     if (!g) return NG_EINVAL;
-    if (g->phase < CAPTURED || !g->rt->d_records) return g->fail(NG_ESTATE, "ng_resident_trace: call ng_capture first");
+    if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_resident_trace: call ng_capture first");
+    if (!g->rt->d_records) return g->fail(NG_ESTATE, "ng_resident_trace: %s", kNoResidentPlan);
     Runtime& rt = *g->rt;
     // the kernel keeps three readings per list entry; a node's figures are the extremes over its entries
     const size_t n = g->nodes.size(), entries = rt.entry_task.size(), bytes = std::max<size_t>(entries, 1) * 3 * sizeof(unsigned long long);

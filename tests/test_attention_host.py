@@ -72,7 +72,8 @@ def test_attention_shapes_and_refusals():
         g.refused(B.NG_EINVAL, "attention_rows node of dy", op, ["dy", y, "q", "k", "v"], **how)
         g.refused(B.NG_EINVAL, "takes dy, rows", op, ["dy", rows, "q", "k"], **how)
     for bad in (dict(heads=4, kv_heads=3), dict(heads=0, kv_heads=1), dict(heads=4, kv_heads=0), dict(heads=4, kv_heads=-2), dict(heads=4, kv_heads=2, scale=float("inf")),
-                dict(heads=4, kv_heads=2, scale=float("nan")), dict(heads=4, kv_heads=2, scale=0.0)):
+                dict(heads=4, kv_heads=2, scale=float("nan")), dict(heads=4, kv_heads=2, scale=0.0),
+                dict(heads=4, kv_heads=2, scale=3e38)):        # finite, but not times log2 e
         g.refused(B.NG_EINVAL, "attention", att, ["q", "k", "v"], **bad)
     g.refused(B.NG_ESHAPE, "128", att, ["big", "big", "big"], heads=2, kv_heads=2)
     g.refused(B.NG_ESHAPE, "heads must divide", att, ["q", "k", "v"], heads=5, kv_heads=5)
@@ -143,3 +144,23 @@ def test_work_of_attention():
     r = g.add(B.NG_OP_HEAD_ROPE, ["q", "pos"], 2, heads=4)
     assert B.ng_task_work(g.g, r)[0] == 4 * (2 * 320 + 5)
     B.ng_destroy(g.g)
+
+
+def test_device_resident_plan_of_attention():
+    """Small tasks have a plan; a graph with kernels that the attention build does not have is refused rather than planned."""
+    few = G(q=(1, 64, 1, 8), k=(1, 64, 1, 300), pos=(1, 1, 1, 8))
+    y = few.add(B.NG_OP_HEAD_ROPE, ["q", "pos"], 1, heads=2)
+    few.add(B.NG_OP_ATTENTION, [y, "k", "k"], heads=2, kv_heads=2)
+    many = G(q=(1, 64, 1, 2048), k=(1, 64, 1, 2048))
+    many.add(B.NG_OP_ATTENTION, ["q", "k", "k"], heads=2, kv_heads=2)
+    for g, planned in ((few, True), (many, False)):
+        B.ng_mark_output(g.g, B.ng_num_nodes(g.g) - 1)
+        B.ng_schedule(g.g)
+        B.ng_plan_memory(g.g)
+        if planned:
+            assert B.ng_resident_dry_plan(g.g)["ok"]
+        else:
+            with pytest.raises(B.NgError) as e:
+                B.ng_resident_dry_plan(g.g)
+            assert e.value.code == B.NG_ESTATE and "no device-resident plan" in str(e.value)
+        B.ng_destroy(g.g)
