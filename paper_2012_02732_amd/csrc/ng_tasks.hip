@@ -232,7 +232,14 @@ static int pair_kid(const Task& first, const Task& second) {
     if (kid_first == KID_ROPE_DX_N && kid_second == KID_ROPE_DG_N) return KID_ROPE_BOTH_N;
     return KID_NONE;
 }
-bool can_pair(const Task& first, const Task& second) { return pair_kid(first, second) != KID_NONE; }
+bool can_pair(const Task& first, const Task& second) {
+    const int kid = pair_kid(first, second);
+    if (kid != KID_ATTN_DKV_T64) return kid != KID_NONE;
+    AttnArgs a, b;                                             // its workgroups are cut in one way for both
+    std::memcpy(&a, first.args, sizeof a);
+    std::memcpy(&b, second.args, sizeof b);
+    return a.col_blocks == b.col_blocks && a.splits == b.splits && a.per_split == b.per_split;
+}
 // The kernel of the launch of task v with everything that rides on it (`fused_into` as decided).
 int launch_kid(const std::vector<Task>& tasks, const std::vector<int>& fused_into, int v) {
     for (size_t w = 0; w < tasks.size(); ++w) {
@@ -644,6 +651,29 @@ struct AttentionPlan {
     size_t ws_floats = 0, cnt_words = 0, stats_floats = 0;
 };
 bool is_attention_op(int op) { return op >= NG_OP_ATTENTION && op <= NG_OP_ATTENTION_DV; }
+// Splits of a tile kernel's other side: the number with which the task is expected to end first. A compute unit has two workgroups at a
+// time, which take longer than one alone, but not twice as long; a last one that is left over has it to itself. A split costs what the
+// workgroup that joins them reads. us, of the straight lines through what these kernels take with 1 .. 32 splits: 47 queries of 28 heads
+// of 128 channels, 9950 keys, 6 splits 127, 8 102, 16 92, 24 128; dq of 175 queries of 120 heads on 30, 660 keys, 1 100, 2 78, 3 95, 8 98; dk of
+// 93 keys of 13 heads of 96, 6892 queries each, 8 127, 16 80, 32 86.
+long tile_splits(int op, bool narrow, long groups, long blocks) {
+    const bool by_keys = op == NG_OP_ATTENTION_DK || op == NG_OP_ATTENTION_DV, both = by_keys && narrow;      // both: one launch, cut alike
+    const bool heavy = !narrow && (op == NG_OP_ATTENTION_DQ || op == NG_OP_ATTENTION_DK);
+    const double one = heavy ? 4.4 : both ? 3.4 : 2.0;             // a block of a workgroup that is alone
+    const double pair = heavy ? 5.8 : both ? 4.4 : narrow ? 2.5 : 3.2;      // of two
+    const double around = heavy ? 8.0 : 6.0;                       // first loads, results
+    const double join = both ? 8.0 : op == NG_OP_ATTENTION ? 6.0 : 4.0, join_each = both ? 1.1 : narrow ? 0.4 : op == NG_OP_ATTENTION ? 0.8 : 0.6;
+    long best = 1;
+    double least = 0;
+    for (long want = 1; want <= std::min<long>(blocks, kMaxSplits); ++want) {
+        const long each = ceil_div(blocks, want), splits = ceil_div(blocks, each), turns = ceil_div(groups * splits, 256);
+        const double us = (double)(turns / 2) * ((double)each * pair + around) + (double)(turns % 2) * ((double)each * one + around) +
+                          (splits > 1 ? join + join_each * (double)splits : 0.0);
+        if (want == 1 || us < least) best = want, least = us;
+    }
+    return best;
+}
+
 AttentionPlan attention_plan(const ng_graph* g, int v) {
     AttentionPlan p;
     const Node& nd = g->nodes[v];
@@ -656,7 +686,7 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     p.kid = nd.op == NG_OP_ATTENTION ? (narrow ? KID_ATTN_W64 : KID_ATTN_W128) : nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_W64 : KID_ATTN_DQ_W128)
           : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_W64 : KID_ATTN_DK_W128) : (narrow ? KID_ATTN_DV_W64 : KID_ATTN_DV_W128);
     const long columns = by_keys ? Tk : group * Tq;
-    long per_block = 16, other = 64, few = 4, workgroups = 1024;   // columns of a workgroup, the other side's in a block, blocks a split has at least
+    long per_block = 16, other = 64, few = 4;                  // columns of a workgroup, the other side's in a block, blocks a split has at least
     // Straight from memory with 16 columns a wavefront, or 128 columns a workgroup through LDS. The former where there are few
     // columns, and where the whole task is a wavefront and block for each of at most 768 wavefronts, three on a compute unit, which
     // then takes as long as one block. Forward, us straight / through LDS: 256 x 256 with one head 7.0 / 13.4 (64 wavefronts), 128 x 77
@@ -667,24 +697,19 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     const bool tiles = columns > 32 && (wavefronts > 768 || (by_keys && narrow));
     if (nd.op == NG_OP_ATTENTION && tiles) {
         p.kid = narrow ? KID_ATTN_T64 : KID_ATTN_T128;
-        per_block = kAttentionColumns, other = narrow ? attention_block<64>() : attention_block<128>(), few = 2, workgroups = 512;
+        per_block = kAttentionColumns, other = narrow ? attention_block<64>() : attention_block<128>(), few = 1;
     } else if (tiles) {
         p.kid = nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_T64 : KID_ATTN_DQ_T128) : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_T64 : KID_ATTN_DK_T128)
               : (narrow ? KID_ATTN_DV_T64 : KID_ATTN_DV_T128);
-        per_block = kAttentionColumns, other = kGradientBlock, few = 2, workgroups = 512;
+        per_block = kAttentionColumns, other = kGradientBlock, few = 1;
     }
     p.col_blocks = (int)ceil_div(columns, per_block);
     const long groups = q.n * nd.p.kv_heads * p.col_blocks, blocks = by_keys ? group * ceil_div(Tq, other) : ceil_div(Tk, other);
-    long want = std::max<long>(1, std::min<long>(ceil_div(blocks, few), ceil_div(workgroups, groups)));
-    if (per_block == kAttentionColumns) {
-        // A block costs a workgroup 2 (64 channels) to 4 us, a split what the workgroup that joins them reads, 0.4 and 1 us: the sum is
-        // smallest near these many. dq of 64 queries of four heads of 64 channels, 4096 keys: 8 splits 42, 16 29, 32 25 us; 16 heads of 128, 100
-        // queries, 4000 keys: 8 82, 16 59, 32 80; without splits 255 and 498.
-        want = std::min<long>({want, kMaxSplits, std::max<long>(1, std::lround(std::sqrt((narrow ? 5.0 : 3.0) * (double)blocks)))});
-        few = 1;
-    } else {
-        want = std::min<long>({want, kMaxWaveSplits, std::max<long>(1, std::lround(std::sqrt(6.0 * (double)blocks)))});
-    }
+    long want = 1;
+    if (per_block == kAttentionColumns)
+        want = tile_splits(nd.op, narrow, groups, blocks);
+    else                                                       // up to 1024 workgroups
+        want = std::max<long>(1, std::min<long>({ceil_div(blocks, few), ceil_div(1024, groups), kMaxWaveSplits, std::lround(std::sqrt(6.0 * (double)blocks))}));
     want = knob_int("NG_ATTN_SPLITS", 1, 32, want);
     p.per_split = (int)(ceil_div(ceil_div(blocks, want), few) * few);
     p.splits = (int)ceil_div(blocks, p.per_split);
