@@ -328,6 +328,18 @@ def test_attention_on_both_sides_of_the_choice_of_kernels(case):
     check_attention(run(g)[B.NG_MODE_GRAPH_SINGLE], q, k, v, dy, ln, heads, kv_heads, d ** -0.5, case)
 
 
+@pytest.mark.parametrize("case", [(1, 4, 4, 64, 40, 5000, None), (1, 3, 3, 128, 47, 3100, "ragged"), (1, 16, 2, 96, 500, 93, None), (2, 8, 1, 48, 700, 60, "odd"),
+                                  (9, 5, 5, 32, 130, 140, "ragged")], ids=str)
+def test_attention_cut_into_many_splits(case):
+    """Few columns against a long other side (32 splits at most), and so many columns that one or two are best."""
+    n, heads, kv_heads, d, tq, tk, kind = case
+    q, k, v, dy, ln = attention_inputs(tq + tk, n, heads, kv_heads, d, tq, tk, kind)
+    g = attention_graph(q, k, v, dy, ln, heads, kv_heads, d ** -0.5)
+    got = run(g)
+    for mode, tensors in got.items():
+        check_attention(tensors, q, k, v, dy, ln, heads, kv_heads, d ** -0.5, (case, mode))
+
+
 @pytest.mark.parametrize("dy_size,v_size", [(1e-20, 1e-11), (1e-33, 1.0), (1e-3, 1e-30)])
 def test_attention_gradients_of_small_products(dy_size, v_size):
     """<dy, v> far below one, but a normal number: 2^-100 and less."""
