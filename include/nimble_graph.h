@@ -356,7 +356,9 @@ int ng_graph_multi_recheck(ng_graph* g, int replays);
 int ng_graph_multi_distrust(ng_graph* g);
 /* Asynchronous: enqueue one inference on the origin stream (hip_streams[0]). */
 int ng_replay(ng_graph* g);
-/* Wait until the origin stream is idle. */
+/* Wait until the origin stream is idle. NG_EHIP if a device-resident replay gave up (ng_resident_config): said at every call until
+ * the next replay, of any mode, is enqueued; a replay that follows one that gave up without a call in between is complete, and the
+ * next call reports the one before it. */
 int ng_sync(ng_graph* g);
 /* The device-resident replay (NG_MODE_DEVICE_RESIDENT, whatever mode is selected) for callers that
  * cannot allocate: code under HIP graph capture, tight serving loops, harnesses that forbid
@@ -377,7 +379,7 @@ int ng_replay_static(ng_graph* g);
  * only before ng_capture) the streams are spread over; with 1 the whole DAG runs out of one
  * XCD's L2 and no completion needs a device-scope fence. spin_limit: polls after which a waiting workgroup
  * gives up (0 = default, a few seconds); every wait in the resident kernel is bounded by it.
- * When a wait gives up, all workgroups leave, ng_sync returns NG_EHIP and the next replay
+ * When a wait gives up, all workgroups leave, ng_sync returns NG_EHIP and the next replay, in whatever mode,
  * starts from clean counters. device_scope_everywhere != 0 (only before ng_capture) makes
  * every completion a device-scope release/acquire; by default a tensor that stays on the
  * XCD of its stream is handed over through that XCD's L2 and only the others pay for an L2

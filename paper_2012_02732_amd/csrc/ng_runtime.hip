@@ -51,7 +51,10 @@ struct Runtime {
     size_t done_words = 0;
     int xcds = 0;
     double est_us = 0;
-    bool counters_dirty = false;
+    bool counters_dirty = false;           // the completion counts start over with the next device-resident replay
+    bool arrivals_dirty = false;           // the arrival counts of the tasks' kernels start over with the next replay in any mode
+    int gave_up = 0;                       // why a device-resident replay gave up (h_error), until ng_sync has said so and another replay starts
+    bool gave_up_reported = false;
     int device = -1;                       // the device that was current at ng_bind
     // a graph that trains: copies of the weights its update nodes write, taken when ng_capture starts
     std::vector<std::pair<float*, size_t>> trained;   // (caller's buffer, elements)
@@ -540,24 +543,52 @@ int tune_resident(ng_graph* g) {
     return rc;
 }
 
-// A replay that gave up may have left workgroups of a task uncounted: the counts of those that whoever is last adds up start over.
-int clear_arrival_counters(ng_graph* g) {
-    for (int v = 0; v < (int)g->nodes.size(); ++v)
-        if (has_arrival_counters(g->nodes[v].op) && g->packed_of[v])
-            if (int rc = pack_constants(g, v, g->packed_of[v], g->rt->streams[0])) return rc;
-    return NG_OK;
+// A device-resident replay has raised the host's flag and ng_sync has not looked since.
+bool flag_is_up(const Runtime& rt) { return rt.h_error && *static_cast<volatile int*>(rt.h_error) != 0; }
+
+// Takes the host's flag down and keeps what it said. Only when the origin stream is idle: a workgroup of a replay that is giving up may
+// raise it again until the replay has ended.
+void take_flag(Runtime& rt) {
+    if (!flag_is_up(rt)) return;
+    rt.gave_up = *static_cast<volatile int*>(rt.h_error), rt.gave_up_reported = false;
+    *rt.h_error = 0;
+    rt.counters_dirty = rt.arrivals_dirty = true;
+}
+
+// A device-resident replay that gave up may have left workgroups of a task uncounted. Kernels whose last workgroup adds up what all of
+// them left (split attention, gradients of weights) would take another one for the last from then on, in this mode and in all the
+// others, which launch the same tasks: their counts start over before the next replay, on its stream, behind the one that gave up.
+int clear_arrivals(ng_graph* g) {
+    Runtime& rt = *g->rt;
+    int dev = -1, rc = NG_OK;                                   // (a graph launch does not ask which device is current, these kernels do)
+    NG_HIP(hipGetDevice(&dev));
+    if (dev != rt.device) NG_HIP(hipSetDevice(rt.device));
+    for (int v = 0; v < (int)g->nodes.size() && rc == NG_OK; ++v)
+        if (has_arrival_counters(g->nodes[v].op) && g->packed_of[v]) rc = pack_constants(g, v, g->packed_of[v], rt.streams[0]);
+    if (dev != rt.device) NG_HIP(hipSetDevice(dev));
+    rt.arrivals_dirty = rt.arrivals_dirty && rc != NG_OK;
+    return rc;
+}
+// Before tasks are launched, by a replay or by themselves.
+int arrivals_ready(ng_graph* g) { return g->rt->arrivals_dirty || flag_is_up(*g->rt) ? clear_arrivals(g) : NG_OK; }
+// Before a replay in any mode. What ng_sync has not yet reported stays to be reported.
+int begin_replay(ng_graph* g) {
+    Runtime& rt = *g->rt;
+    if (rt.gave_up_reported) rt.gave_up = 0, rt.gave_up_reported = false;
+    return arrivals_ready(g);
 }
 
 int launch_resident(ng_graph* g) {
     Runtime& rt = *g->rt;
     if (!rt.d_records) return g->fail(NG_ESTATE, "device-resident replay: %s", kNoResidentPlan);
     hipStream_t origin = rt.streams[0];
-    if (rt.counters_dirty) {                                   // a timed-out replay left partial counts behind
+    if (rt.counters_dirty || flag_is_up(rt)) {                 // a replay that gave up left partial counts behind
         NG_HIP(hipStreamSynchronize(origin));
+        take_flag(rt);
         NG_HIP(hipMemsetAsync(rt.plan.done, 0, (10 * rt.done_words + 18) * sizeof(unsigned), origin));   // on the stream of the launch below
         NG_HIP(hipMemsetAsync(rt.plan.error_dev, 0, sizeof(int), origin));
-        if (int rc = clear_arrival_counters(g)) return rc;
-        *rt.h_error = 0;
+        if (rt.arrivals_dirty)
+            if (int rc = clear_arrivals(g)) return rc;
         rt.epoch = 0;
         rt.counters_dirty = false;
     }
@@ -745,6 +776,7 @@ int ng_capture(ng_graph* g) {
         if (rt.exec[i]) (void)hipGraphExecDestroy(rt.exec[i]), rt.exec[i] = nullptr;
         if (rt.graph[i]) (void)hipGraphDestroy(rt.graph[i]), rt.graph[i] = nullptr;
     }
+    if (int rc = arrivals_ready(g)) return rc;                 // (an earlier ng_capture may have ended with a replay that gave up)
     if (g->trainable)
         if (int rc = save_trained_weights(g)) return rc;
     if (int rc = record_multi(g, 0)) return rc;
@@ -823,6 +855,7 @@ int ng_graph_multi_recheck(ng_graph* g, int replays) {
     if (g->graph_multi_state < 0) return NG_OK;               // a mismatch once seen stays
     Runtime& rt = *g->rt;
     NG_HIP(hipStreamSynchronize(rt.streams[0]));
+    if (int rc = arrivals_ready(g)) return rc;
     if (g->trainable)
         if (int rc = save_trained_weights(g)) return rc;
     int rc = verify_graph_multi(g, replays);
@@ -861,6 +894,7 @@ int ng_replay(ng_graph* g) {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_replay: call ng_capture first");
     Runtime& rt = *g->rt;
+    if (int rc = begin_replay(g)) return rc;
     switch (g->mode == NG_MODE_AUTO ? g->auto_mode : g->mode) {
         case NG_MODE_GRAPH_MULTI:
             if (g->graph_multi_state < 0)
@@ -929,9 +963,7 @@ int ng_replay_static(ng_graph* g) {
     plan.trace = nullptr;
     plan.spin_limit = g->resident_spin_limit;
     hipStream_t origin = rt.streams[0];
-    if (*rt.h_error != 0) *rt.h_error = 0;                     // left by a replay that gave up (calls do not overlap, so it has ended)
-    if (rt.counters_dirty)
-        if (int rc = clear_arrival_counters(g)) return rc;
+    if (int rc = begin_replay(g)) return rc;
     const unsigned blocks = (unsigned)std::min<size_t>((need + 255) / 256, 1024);
     zero_words_kernel<<<dim3(blocks), dim3(256), 0, origin>>>(base, need);
     NG_HIP(hipGetLastError());
@@ -945,10 +977,12 @@ int ng_sync(ng_graph* g) {
     if (!g) return NG_EINVAL;
     if (g->phase < BOUND) return g->fail(NG_ESTATE, "ng_sync: call ng_bind first");
     NG_HIP(hipStreamSynchronize(g->rt->streams[0]));
-    if (g->rt->h_error && *g->rt->h_error != 0) {
-        const int task = *g->rt->h_error - 1;
-        g->rt->counters_dirty = true;
-        if (*g->rt->h_error == kErrorXcdMapping)
+    Runtime& rt = *g->rt;
+    take_flag(rt);
+    if (rt.gave_up != 0) {
+        const int task = rt.gave_up - 1;
+        rt.gave_up_reported = true;
+        if (rt.gave_up == kErrorXcdMapping)
             return g->fail(NG_EHIP, "device-resident replay: workgroups with equal index mod 8 did not share an XCD in this launch, which the "
                                     "plan's use of XCD-local L2s rests on; outputs may be stale");
         return g->fail(NG_EHIP, "device-resident replay: the wait before task %d ran out of spins; outputs are incomplete", task);
@@ -1063,6 +1097,7 @@ static int chain_time(ng_graph* g, const void* fn, const unsigned grid[3], const
                       void* arg_block, int reps, float* us_per_node) {
     Runtime& rt = *g->rt;
     hipStream_t s = rt.streams[0];
+    if (int rc = arrivals_ready(g)) return rc;
     hipGraph_t graph = nullptr;
     hipGraphExec_t exec = nullptr;
     NG_HIP(hipGraphCreate(&graph, 0));
@@ -1221,6 +1256,7 @@ int ng_time_task_device(ng_graph* g, int id, int as_executed, int reps, float* m
     void* args[2] = {l.args.data(), &stamps};
     std::vector<unsigned long long> h(2 * wgs);
     std::vector<float> us;
+    if (int rc = arrivals_ready(g)) return rc;
     NG_HIP(hipStreamSynchronize(s));
     for (int rep = -2; rep < reps; ++rep) {                        // two untimed launches first
         NG_HIP(hipLaunchKernel(l.timed_fn, l.grid, l.block, args, l.lds_bytes, s));
@@ -1249,6 +1285,7 @@ int ng_launch_task_solo(ng_graph* g, int id, int as_executed) {
         SoloLaunch l = solo_launch(g->tasks[id]);
         if (as_executed && !executed_launch(g, id, g->mode, l)) return NG_OK;
         if (!l.fn) return NG_OK;
+        if (int rc = arrivals_ready(g)) return rc;
         void* args[1] = {l.args.data()};
         NG_HIP(hipLaunchKernel(l.fn, l.grid, l.block, args, l.lds_bytes, s));
     }
