@@ -96,7 +96,9 @@ enum {
                                    (a, b) -> factor (a cos t - b sin t, a sin t + b cos t), t = position * frequencies[i], for the
                                  pairs i < rot / 2 of the head's first rot channels (rot even, 2 .. d): channels (2 i, 2 i + 1) if
                                  interleaved != 0, else (i, i + rot / 2); the channels from rot on are u. positions: [1][1] or
-                                 [n][1] x tokens of x, any finite numbers; no gradient goes to them */
+                                 [n][1] x tokens of x, finite, fractions and negative ones as well; |position * frequency| up to 2^72
+                                 is reduced to a turn within 2^-34 of it (beyond that less and less is left of the angle); no gradient
+                                 goes to them */
     NG_OP_HEAD_ROPE_DGRAD = 26, /* preds {dy, x, positions}, same weights and parameters -> dx */
     NG_OP_HEAD_ROPE_WGRAD = 27, /* preds {dy, x, positions}, weights {frequencies, gamma} -> dgamma as [1][d][1][1] */
     NG_OP_ATTENTION = 28,     /* preds {q, k, v} or {q, k, v, lengths}, no weights. q has c = heads d channels and Tq tokens, k and v

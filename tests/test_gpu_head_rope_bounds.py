@@ -1,4 +1,4 @@
-"""Norm and rotation of heads on the GPU: channels that are passed through."""
+"""Norm and rotation of heads on the GPU: channels that are passed through, and angles of far positions."""
 import numpy as np
 import pytest
 
@@ -50,3 +50,18 @@ def test_gradient_of_gamma_next_to_infinities(tokens):
     others = [c for c in range(16) if c != 9]
     # a sum of 4 tokens terms of order one
     assert np.abs(got - clean)[0, others].max() <= 4 * U * 4 * tokens
+
+
+@pytest.mark.parametrize("tokens", [4, 64])
+@pytest.mark.parametrize("base", [1e3, 2.0 ** 24, 2.0 ** 40, 2.0 ** 60])
+def test_angles_of_far_positions(base, tokens):
+    """The rotation of unit vectors shows the angle itself. Its fraction of a turn is known to far below 2^-32, so what is left is the
+    rounding of sine and cosine (two steps at most) and of the products: 6 u."""
+    rng = np.random.default_rng(tokens)
+    x = np.zeros((1, 128, 1, tokens), np.float32)
+    x[:, :64] = 1.0
+    pos = (base * rng.uniform(0.5, 1.0, (1, 1, 1, tokens))).astype(np.float32)
+    args = (x, pos, rope_frequencies(128), None, x, 1, 0, 0.0, 1.0)
+    got, ref = run(rope_graph(*args))[B.NG_MODE_GRAPH_SINGLE], rope_reference(*args)
+    for name in ref:
+        assert np.abs(got[name] - ref[name]).max() <= 6 * U, (name, np.abs(got[name] - ref[name]).max() / U)
