@@ -112,8 +112,8 @@ enum {
                                  the largest magnitude of a query, of a key head's keys, of its values (gradients: also of dy): 2^-13 of it
                                  and more has all its bits, down to 2^-37 fewer and fewer, less is 0 */
     NG_OP_ATTENTION_ROWS = 29, /* preds {dy, y}, y an NG_OP_ATTENTION node, heads as there -> [n][3 heads] x tokens of y: for each query
-                                 <dy, y> of its head, a reference near the largest score (times log2 e) of its keys, and one over
-                                 the sum of their 2^(score log2 e - reference); 0 and 0 without any key. What the three gradients need of every query */
+                                 <dy, y> of its head, a reference score (times log2 e) and a factor from 1 to 2 with which its weights are
+                                 factor 2^(score log2 e - reference); 0 and 0 without any key. What the three gradients need of every query */
     NG_OP_ATTENTION_DQ = 30,  /* preds {dy, rows, q, k, v[, lengths]} of one attention, heads, kv_heads and scale as there; rows: its */
     NG_OP_ATTENTION_DK = 31,  /* NG_OP_ATTENTION_ROWS node -> dq, dk (shapes of q, k; 0 for keys that do not count) */
     NG_OP_ATTENTION_DV = 32   /* -> dv */

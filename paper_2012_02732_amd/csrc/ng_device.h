@@ -421,7 +421,7 @@ struct AttnArgs {
     const float* dy;           // gradients
     const float* rows;         // gradients: [n][3][H][Tq]
     float* y;                  // the result: y, dq, dk or dv
-    float* stats;              // forward: [2][n][H][Tq] largest score, one over the sum (nullptr: nobody reads them); rows: read
+    float* stats;              // forward: [2][n][H][Tq] reference score and factor of a query (attention_stats; nullptr: nobody reads them); rows: read
     float* ws;                 // splits > 1: partial results of each split
     unsigned* cnt;             // splits > 1: arrivals for each block of the result, zero between replays
     float scale, scale_log2;   // scale_log2 = scale log2 e
