@@ -119,3 +119,20 @@ def test_dv_of_queries_with_sharp_and_with_even_weights():
     q[:, 1, :, ::2], k[:, 1, :, 0] = 8.0, 64.0
     dy[:, :, :, ::2] *= 2.0 ** 12
     checked(q, k, v, dy, ln, 1, 1, 0.125, TILE_64, "sharp and even")
+
+
+def test_attention_of_zero_queries_with_a_tiny_scale():
+    """Queries of zeros weigh all keys alike whatever the scale is; the last block has keys that do not exist."""
+    for d, names in ((64, TILE_64), (128, TILE_128)):
+        q, k, v, dy, ln = attention_inputs(51, 2, 8, 4, d, 150, 333, None)
+        q[:, :, :, ::3] = 0.0
+        k[:, : d] = 0.0
+        checked(q, k, v, dy, ln, 8, 4, 1e-9, names, d)
+
+
+@pytest.mark.parametrize("q_size,k_size,scale_size", [(2.0 ** -60, 2.0 ** -50, 2.0 ** 110), (2.0 ** -70, 2.0 ** -50, 2.0 ** 120), (2.0 ** 60, 2.0 ** 50, 2.0 ** -110)])
+def test_attention_of_products_that_the_scale_makes_up_for(q_size, k_size, scale_size):
+    for d, names in ((64, TILE_64), (128, TILE_128)):
+        q, k, v, dy, ln = attention_inputs(61, 2, 8, 4, d, 150, 333, None)
+        q, k = q * np.float32(q_size), k * np.float32(k_size)
+        checked(q, k, v, dy, ln, 8, 4, d ** -0.5 * scale_size, names, (d, q_size))
