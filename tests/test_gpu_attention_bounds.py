@@ -136,3 +136,12 @@ def test_attention_of_products_that_the_scale_makes_up_for(q_size, k_size, scale
         q, k, v, dy, ln = attention_inputs(61, 2, 8, 4, d, 150, 333, None)
         q, k = q * np.float32(q_size), k * np.float32(k_size)
         checked(q, k, v, dy, ln, 8, 4, d ** -0.5 * scale_size, names, (d, q_size))
+
+
+@pytest.mark.parametrize("case,names", [((1, 4, 4, 64, 40, 5000), TILE_64), ((1, 4, 1, 128, 33, 6000), TILE_128), ((2, 8, 4, 128, 150, 333), TILE_128)], ids=str)
+def test_attention_of_values_next_to_the_largest(case, names):
+    """Weighted means of values of 2^120: no sum on the way leaves fp32's range, cut into splits or not."""
+    n, heads, kv_heads, d, tq, tk = case
+    q, k, v, dy, ln = attention_inputs(71, n, heads, kv_heads, d, tq, tk, None)
+    v = (np.abs(v) * 2.0 ** 120).astype(np.float32)
+    checked(q, k, v, None, ln, heads, kv_heads, d ** -0.5, names, case)
