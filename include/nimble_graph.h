@@ -108,9 +108,10 @@ enum {
                                  image b has the keys j < lengths[b] (not a number: none), whatever lies behind them in k and v;
                                  y[i] = sum_j p[i][j] v[j], p[i][.] = softmax over these keys of scale <q[i], k[j]>; a query
                                  without any key: 0. q, and the keys and values that count, have to be finite, scale log2 e too.
-                                 Sums in fp32. With many columns the factors of a product are two half-precision parts in a unit of
-                                 the largest magnitude of a query, of a key head's keys, of its values (gradients: also of dy): 2^-13 of it
-                                 and more has all its bits, down to 2^-37 fewer and fewer, less is 0 */
+                                 Sums in fp32 (values of up to 2^127 over the number of keys). With many columns the factors of a product
+                                 are two half-precision parts in a unit of the largest magnitude of a query, of a key head's keys, of its
+                                 values (gradients: also of dy): 2^-13 of it and more has all its bits, down to 2^-37 fewer and fewer,
+                                 less is 0 (ng_set_unsplit_products: never so) */
     NG_OP_ATTENTION_ROWS = 29, /* preds {dy, y}, y an NG_OP_ATTENTION node, heads as there -> [n][3 heads] x tokens of y: for each query
                                  <dy, y> of its head, a reference score (times log2 e) and a factor from 1 to 2 with which its weights are
                                  factor 2^(score log2 e - reference); 0 and 0 without any key. What the three gradients need of every query */
@@ -242,6 +243,12 @@ int ng_set_memory_reuse(ng_graph* g, int on);
  * same kernel that do not wait for each other share a launch as well, and the launches follow each other in an
  * order that lets them (ng_get_single_launches). on = 0 switches the exceptions off: one kernel per task. Call before ng_bind (NG_ESTATE after). */
 int ng_set_launch_fusion(ng_graph* g, int on);
+/* How NG_OP_ATTENTION and its gradients multiply. By default a task of many columns takes its factors as two half-precision
+ * parts in units of a query's or of a whole head matrix's largest magnitude (see NG_OP_ATTENTION): fp32's accuracy where magnitudes are
+ * within 2^13 of the largest, less for a channel or token that is smaller. on = 1: every product of two fp32 values as one, whatever
+ * their sizes, by the kernels that tasks of few columns have anyway; 4096 x 4096 tokens, 32 heads of 128 channels on 8, take 3.0 ms instead of
+ * 0.85, a training step 2048 x 2048 of 16 heads on 4, two images, 5.7 instead of 1.2. Call before ng_bind (NG_ESTATE after). */
+int ng_set_unsplit_products(ng_graph* g, int on);
 /* offset[n_nodes], bytes[n_nodes] of each node's output inside the arena (host arrays). */
 int ng_get_offsets(const ng_graph* g, size_t* offset, size_t* bytes);
 

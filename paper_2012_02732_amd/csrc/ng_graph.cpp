@@ -544,6 +544,13 @@ int ng_set_launch_fusion(ng_graph* g, int on) {
     return NG_OK;
 }
 
+int ng_set_unsplit_products(ng_graph* g, int on) {
+    if (!g) return NG_EINVAL;
+    if (g->phase >= BOUND) return g->fail(NG_ESTATE, "ng_set_unsplit_products: the task table is already built");
+    g->unsplit_products = on != 0;
+    return NG_OK;
+}
+
 int ng_get_offsets(const ng_graph* g, size_t* offset, size_t* bytes) {
     if (!g) return NG_EINVAL;
     if (g->phase < PLANNED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_get_offsets: call ng_plan_memory first");

@@ -144,6 +144,7 @@ struct ng_graph {
     int mode = NG_MODE_AUTO;
     bool trainable = false;                              // some node updates weights: nothing derived from weight values may be kept across replays
     bool launch_fusion = true;                           // modes 0-3: batch-norm / ReLU applied by the convolution's kernel, in-place concats not launched
+    bool unsplit_products = false;                          // attention: no products of half-precision parts
     int graph_multi_state = 0;                           // capture-time check of the multi-stream graph: 0 not run, 1 reproduced the single-stream result, -1 did not
     int graph_multi_checked = 0;                         // replays of it that were compared
     int assignment = NG_ASSIGN_ALGORITHM1;               // how ng_schedule forms the streams

@@ -694,7 +694,7 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     // 64 heads 17.5 / 8.9 (2048); dq 12.4 / 13.3, 11.8 / 13.6, 24.4 / 29.5, 23.5 / 12.3, 19.6 / 12.6. dk and dv share a launch through LDS with up
     // to 64 channels; with more, 128 x 128 with four heads 21 + 15 / 24 + 18 (64), 48 x 512 with 32 heads 49 + 35 / 18 + 13 (1024).
     const long wavefronts = q.n * nd.p.kv_heads * ceil_div(columns, 16) * (by_keys ? group * ceil_div(Tq, 64) : ceil_div(Tk, 64));
-    const bool tiles = columns > 32 && (wavefronts > 768 || (by_keys && narrow));
+    const bool tiles = !g->unsplit_products && columns > 32 && (wavefronts > 768 || (by_keys && narrow));
     if (nd.op == NG_OP_ATTENTION && tiles) {
         p.kid = narrow ? KID_ATTN_T64 : KID_ATTN_T128;
         per_block = kAttentionColumns, other = narrow ? attention_block<64>() : attention_block<128>(), few = 1;

@@ -140,14 +140,17 @@ class GraphRunner:
 
     # -- GPU part ----------------------------------------------------------------
     def prepare(self, resident_wg_per_cu=0, resident_xcds=0, resident_device_scope=0, plan_trials=None, launch_fusion=True,
-                origin_stream=None):
+                origin_stream=None, unsplit_products=False):
         """schedule -> plan -> bind -> capture, allocating arena and streams with torch. ``origin_stream``: the handle of a
-        stream of the caller's (not the null stream) that replays are enqueued on, instead of one of this graph's own."""
+        stream of the caller's (not the null stream) that replays are enqueued on, instead of one of this graph's own.
+        ``unsplit_products``: attention never multiplies in half-precision parts (ng_set_unsplit_products)."""
         assert self.device is not None, "GraphRunner was created without a device"
         if plan_trials is not None:
             B.ng_resident_plan_trials(self.g, plan_trials)
         if not launch_fusion:
             B.ng_set_launch_fusion(self.g, False)
+        if unsplit_products:
+            B.ng_set_unsplit_products(self.g, True)
         if resident_wg_per_cu or resident_xcds or resident_device_scope:
             B.ng_resident_config(self.g, resident_wg_per_cu, resident_xcds, 0, resident_device_scope)
         sched = self.schedule()

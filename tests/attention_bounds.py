@@ -73,18 +73,19 @@ def reference_and_rss(q, k, v, dy, ln, heads, kv_heads, scale):
     return ref, rss
 
 
-def excess(got, ref, rss):
-    """{name: the largest |error| of a vector over what it may be}; NaN counts as infinitely far off."""
+def excess(got, ref, rss, axis=2):
+    """{name: the largest |error| of a vector over what it may be}; NaN counts as infinitely far off. axis 3: vectors are not the channels
+    of a token but a channel's values at all tokens."""
     worst = {}
     for name in ref:
         t = np.asarray(got[name], np.float64).reshape(ref[name].shape)
-        off, may = np.sqrt(((t - ref[name]) ** 2).sum(axis=2)), MARGIN * U * np.sqrt((rss[name] ** 2).sum(axis=2))
+        off, may = np.sqrt(((t - ref[name]) ** 2).sum(axis=axis)), MARGIN * U * np.sqrt((rss[name] ** 2).sum(axis=axis))
         worst[name] = float(np.max(np.where(np.isfinite(off), off / np.maximum(may, 1e-300), np.inf)))
     return worst
 
 
 def check(got, q, k, v, dy, ln, heads, kv_heads, scale, what):
     ref, rss = reference_and_rss(q, k, v, dy, ln, heads, kv_heads, scale)
-    worst = excess(got, ref, rss)
-    assert all(w <= 1.0 for w in worst.values()), (what, worst)
-    return worst
+    for axis in (2, 3):
+        worst = excess(got, ref, rss, axis)
+        assert all(w <= 1.0 for w in worst.values()), (what, axis, worst)

@@ -15,9 +15,10 @@ WAVE_64 = {name: kernel.replace("tile", "wave") for name, kernel in TILE_64.item
 WAVE_128 = {name: kernel.replace("64", "128") for name, kernel in WAVE_64.items()}
 
 
-def kernels(g):
+def kernels(g, unsplit_products=False):
     r = GraphRunner(g.workload())
     try:
+        B.ng_set_unsplit_products(r.g, unsplit_products)
         r.schedule()
         r.plan()
         return {name: B.ng_planned_task_kernel(r.g, g.names[name]) for name in ("y", "dq", "dk", "dv") if name in g.names}
@@ -33,14 +34,14 @@ def forward_graph(q, k, v, heads, kv_heads, scale):
     return g
 
 
-def checked(q, k, v, dy, ln, heads, kv_heads, scale, names, what):
+def checked(q, k, v, dy, ln, heads, kv_heads, scale, names, what, unsplit_products=False):
     """Forward and gradients, or without dy the forward operator alone."""
     if dy is None:
         g, names = forward_graph(q, k, v, heads, kv_heads, scale), {"y": names["y"]}
     else:
         g = attention_graph(q, k, v, dy, ln, heads, kv_heads, scale)
-    assert kernels(g) == names, (what, kernels(g))
-    got = run(g)[B.NG_MODE_GRAPH_SINGLE]
+    assert kernels(g, unsplit_products) == names, (what, kernels(g, unsplit_products))
+    got = run(g, unsplit_products=unsplit_products)[B.NG_MODE_GRAPH_SINGLE]
     check(got, q, k, v, dy, ln, heads, kv_heads, scale, what)
     return got
 
@@ -145,3 +146,28 @@ def test_attention_of_values_next_to_the_largest(case, names):
     q, k, v, dy, ln = attention_inputs(71, n, heads, kv_heads, d, tq, tk, None)
     v = (np.abs(v) * 2.0 ** 120).astype(np.float32)
     checked(q, k, v, None, ln, heads, kv_heads, d ** -0.5, names, case)
+
+
+@pytest.mark.parametrize("sizes,names", [((2, 8, 4, 128, 150, 333), WAVE_128), ((2, 8, 4, 64, 150, 333), WAVE_64), ((1, 4, 4, 64, 40, 5000), WAVE_64)], ids=str)
+@pytest.mark.parametrize("powers", [-30, 30])
+def test_unsplit_products_of_channels_of_very_different_size(sizes, names, powers):
+    """Channels 2^0 .. 2^powers as large as the first, made up for in the factor that they meet: with products of fp32 values, of this size
+    too, every vector is as precise as ever (in half-precision parts the small ones lose their bits)."""
+    n, heads, kv_heads, d, tq, tk = sizes
+    q, k, v, dy, ln = attention_inputs(81, n, heads, kv_heads, d, tq, tk, None)
+    each = (2.0 ** np.round(np.linspace(0, powers, d))).astype(np.float32)
+    per_q, per_k = (np.tile(each, m)[None, :, None, None] for m in (heads, kv_heads))
+    checked(q, k, v * per_k, dy / per_q, ln, heads, kv_heads, d ** -0.5, names, (sizes, powers, "values"), unsplit_products=True)
+    checked(q * per_q, k / per_k, v, dy, ln, heads, kv_heads, d ** -0.5, names, (sizes, powers, "keys"), unsplit_products=True)
+
+
+def test_unsplit_products_are_chosen_before_binding():
+    q, k, v, dy, ln = attention_inputs(81, 1, 2, 2, 16, 4, 5, None)
+    r = GraphRunner(attention_graph(q, k, v, dy, ln, 2, 2, 0.25).workload(), "cuda:0")
+    try:
+        r.prepare(plan_trials=1)
+        with pytest.raises(B.NgError) as e:
+            B.ng_set_unsplit_products(r.g, True)
+        assert e.value.code == B.NG_ESTATE
+    finally:
+        r.close()
