@@ -107,13 +107,14 @@ enum {
                                  head i reads key head i / (heads / kv_heads), kv_heads a divisor of heads. lengths [n][1][1][1]:
                                  image b has the keys j < lengths[b] (not a number: none), whatever lies behind them in k and v;
                                  y[i] = sum_j p[i][j] v[j], p[i][.] = softmax over these keys of scale <q[i], k[j]>; a query
-                                 without any key: 0. q, and the keys and values that count, have to be finite, scale log2 e too.
+                                 without any key: 0. q, the keys and values that count, and for the gradients dy have to be finite, scale
+                                 log2 e too (an infinity may take finite results with it, of its matrix too).
                                  Sums in fp32 (values of up to 2^127 over the number of keys). With many columns the factors of a product
                                  are two half-precision parts in a unit of the largest magnitude of a query, of a key head's keys, of its
                                  values (gradients: also of dy): 2^-13 of it and more has all its bits, down to 2^-37 fewer and fewer,
                                  less is 0 (ng_set_unsplit_products: never so) */
     NG_OP_ATTENTION_ROWS = 29, /* preds {dy, y}, y an NG_OP_ATTENTION node, heads as there -> [n][3 heads] x tokens of y: for each query
-                                 <dy, y> of its head, a reference score (times log2 e) and a factor from 1 to 2 with which its weights are
+                                 <dy, y> of its head, a reference score (times log2 e) and a factor from 1/2 to 1 with which its weights are
                                  factor 2^(score log2 e - reference); 0 and 0 without any key. What the three gradients need of every query */
     NG_OP_ATTENTION_DQ = 30,  /* preds {dy, rows, q, k, v[, lengths]} of one attention, heads, kv_heads and scale as there; rows: its */
     NG_OP_ATTENTION_DK = 31,  /* NG_OP_ATTENTION_ROWS node -> dq, dk (shapes of q, k; 0 for keys that do not count) */
@@ -241,7 +242,7 @@ int ng_set_memory_reuse(ng_graph* g, int on);
  * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, and dk and
  * dv of an attention with many keys and heads of up to 64 channels, with what both need computed once. In modes 1 and 2 tasks of the
  * same kernel that do not wait for each other share a launch as well, and the launches follow each other in an
- * order that lets them (ng_get_single_launches). on = 0 switches the exceptions off: one kernel per task. Call before ng_bind (NG_ESTATE after). */
+ * order that lets them (ng_get_single_launches; attention operators' kernels have a launch each). on = 0 switches the exceptions off: one kernel per task. Call before ng_bind (NG_ESTATE after). */
 int ng_set_launch_fusion(ng_graph* g, int on);
 /* How NG_OP_ATTENTION and its gradients multiply. By default a task of many columns takes its factors as two half-precision
  * parts in units of a query's or of a whole head matrix's largest magnitude (see NG_OP_ATTENTION): fp32's accuracy where magnitudes are
