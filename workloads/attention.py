@@ -10,7 +10,7 @@ def decoder_block(seed: int = 0, batch: int = 2, heads: int = 4, kv_heads: int =
                   width: int = 24, state_width: int = 20, lengths=None) -> Workload:
     """Tokens [batch, width, 1, tokens] attend to states [batch, state_width, 1, states] (1 x 1 projections, norm and rotation of
     the heads of queries and keys, heads that share keys, key counts), a residual sum, then to each other (rotated pairs
-    interleaved, a part of the head). Inputs: the tokens, the states, positions of both, the states that count for each image
+    interleaved, a part of the head; no mask: every token reads every other). Inputs: the tokens, the states, positions of both, the states that count for each image
     (``lengths``; default: all but two of the first image's, none of the others')."""
     rng = np.random.default_rng(seed)
     b = Builder("decoder_block")
