@@ -571,11 +571,9 @@ int clear_arrivals(ng_graph* g) {
 }
 // Before tasks are launched, by a replay or by themselves.
 int arrivals_ready(ng_graph* g) { return g->rt->arrivals_dirty || flag_is_up(*g->rt) ? clear_arrivals(g) : NG_OK; }
-// Before a replay in any mode. What ng_sync has not yet reported stays to be reported.
-int begin_replay(ng_graph* g) {
-    Runtime& rt = *g->rt;
+// A replay has been enqueued, in any mode: what ng_sync has reported is over, what it has not stays to be reported.
+void replay_enqueued(Runtime& rt) {
     if (rt.gave_up_reported) rt.gave_up = 0, rt.gave_up_reported = false;
-    return arrivals_ready(g);
 }
 
 int launch_resident(ng_graph* g) {
@@ -890,11 +888,8 @@ int ng_replay_mode(ng_graph* g, int mode) {
     return NG_OK;
 }
 
-int ng_replay(ng_graph* g) {
-    if (!g) return NG_EINVAL;
-    if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_replay: call ng_capture first");
+static int enqueue_replay(ng_graph* g) {
     Runtime& rt = *g->rt;
-    if (int rc = begin_replay(g)) return rc;
     switch (g->mode == NG_MODE_AUTO ? g->auto_mode : g->mode) {
         case NG_MODE_GRAPH_MULTI:
             if (g->graph_multi_state < 0)
@@ -912,6 +907,15 @@ int ng_replay(ng_graph* g) {
         case NG_MODE_EAGER_MULTI: return issue_all(g, true);
         default: return launch_resident(g);
     }
+}
+
+int ng_replay(ng_graph* g) {
+    if (!g) return NG_EINVAL;
+    if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_replay: call ng_capture first");
+    if (int rc = arrivals_ready(g)) return rc;
+    if (int rc = enqueue_replay(g)) return rc;
+    replay_enqueued(*g->rt);
+    return NG_OK;
 }
 
 // ---- device-resident replay that allocates nothing -------------------------------------------
@@ -963,13 +967,14 @@ int ng_replay_static(ng_graph* g) {
     plan.trace = nullptr;
     plan.spin_limit = g->resident_spin_limit;
     hipStream_t origin = rt.streams[0];
-    if (int rc = begin_replay(g)) return rc;
+    if (int rc = arrivals_ready(g)) return rc;
     const unsigned blocks = (unsigned)std::min<size_t>((need + 255) / 256, 1024);
     zero_words_kernel<<<dim3(blocks), dim3(256), 0, origin>>>(base, need);
     NG_HIP(hipGetLastError());
     unsigned epoch = 1;
     void* args[2] = {&plan, &epoch};
     NG_HIP(hipLaunchKernel(resident_kernel_handle(rt.resident_build), dim3(rt.n_wg), dim3(kGroup), args, 0, origin));
+    replay_enqueued(rt);
     return NG_OK;
 }
 

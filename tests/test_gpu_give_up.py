@@ -105,3 +105,50 @@ def test_check_of_the_multi_stream_graph_after_one_that_gave_up():
         r.sync()
     finally:
         r.close()
+
+
+def test_a_refused_replay_does_not_end_the_report():
+    q, k, v, dy, ln = attention_inputs(12, 2, 2, 2, 100, 20, 300, None)
+    r = GraphRunner(attention_graph(q, k, v, dy, ln, 2, 2, 0.25).workload(), DEV)
+    try:
+        r.prepare(plan_trials=1)
+        B.ng_graph_multi_distrust(r.g)
+        give_up(r)
+        for _ in range(2):
+            with pytest.raises(B.NgError) as e:
+                r.sync()
+            assert e.value.code == B.NG_EHIP
+            with pytest.raises(B.NgError) as e:
+                r.replay(B.NG_MODE_GRAPH_MULTI)
+            assert e.value.code == B.NG_ESTATE
+        r.replay(B.NG_MODE_EAGER_SINGLE)
+        r.sync()
+    finally:
+        r.close()
+
+
+@pytest.mark.parametrize("mode", list(MODES))
+def test_gradients_of_convolutions_after_one_that_gave_up(mode):
+    """The sums by last arrival of convolutions, depthwise convolutions and batch-norms; a rate of 0 leaves the weights as they are."""
+    import workloads
+    w = workloads.nas_cell_cifar(batch=4, image=16)
+    out = w.outputs[0]
+    seed = np.random.default_rng(1).standard_normal(w.nodes[out].shape).astype(np.float32)
+    tw = workloads.training_graph(w, 0.0, {out: seed})
+    r = GraphRunner(tw, DEV)
+    try:
+        r.prepare(plan_trials=1)
+        grads = sorted({node for node, _, _ in tw.wgrad_of.values()})
+        replay(r, mode)
+        first = {node: r.output(node) for node in grads}
+        for _ in range(2):
+            give_up(r)
+            with pytest.raises(B.NgError) as e:
+                r.sync()
+            assert e.value.code == B.NG_EHIP
+            for _ in range(2):
+                replay(r, mode)
+                for node in grads:
+                    assert np.array_equal(r.output(node), first[node]), (mode, node, tw.nodes[node].op)
+    finally:
+        r.close()
