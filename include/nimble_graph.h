@@ -366,9 +366,10 @@ int ng_graph_multi_recheck(ng_graph* g, int replays);
 int ng_graph_multi_distrust(ng_graph* g);
 /* Asynchronous: enqueue one inference on the origin stream (hip_streams[0]). */
 int ng_replay(ng_graph* g);
-/* Wait until the origin stream is idle. NG_EHIP if a device-resident replay gave up (ng_resident_config): said at every call until
- * the next replay, of any mode, is enqueued; a replay that follows one that gave up without a call in between is complete, and the
- * next call reports the one before it. */
+/* Wait until the origin stream is idle. NG_EHIP if a device-resident replay gave up (ng_resident_config): its results are incomplete, and
+ * those of replays that were enqueued behind it before it had ended may be. Said at every call until the next replay, of any mode, is
+ * enqueued. A caller that waits by other means gets complete results from the replay after one that gave up, and the report of
+ * the latter from the next call. */
 int ng_sync(ng_graph* g);
 /* The device-resident replay (NG_MODE_DEVICE_RESIDENT, whatever mode is selected) for callers that
  * cannot allocate: code under HIP graph capture, tight serving loops, harnesses that forbid
