@@ -118,7 +118,28 @@ enum {
                                  factor 2^(score log2 e - reference); 0 and 0 without any key. What the three gradients need of every query */
     NG_OP_ATTENTION_DQ = 30,  /* preds {dy, rows, q, k, v[, lengths]} of one attention, heads, kv_heads and scale as there; rows: its */
     NG_OP_ATTENTION_DK = 31,  /* NG_OP_ATTENTION_ROWS node -> dq, dk (shapes of q, k; 0 for keys that do not count) */
-    NG_OP_ATTENTION_DV = 32   /* -> dv */
+    NG_OP_ATTENTION_DV = 32,  /* -> dv */
+    /* Around the attention of a transformer block. */
+    NG_OP_LAYER_NORM = 33,    /* preds {x}, weights {gamma[c], beta[c]}: over the c channels of each pixel (token), y = gamma (x - mean) /
+                                 sqrt(variance + eps) + beta, variance the mean of (x - mean)^2. c h w <= 2^29. (Up to 4096 channels are
+                                 read once, more of them once for each sum.) */
+    NG_OP_LAYER_NORM_DGRAD = 34, /* preds {dy, x}, same weights, eps -> dx */
+    NG_OP_LAYER_NORM_WGRAD = 35, /* preds {dy, x}, same weights, eps -> [2][c][1][1]: dgamma, then dbeta */
+    NG_OP_DROPOUT = 36,       /* preds {x, seed} or {x, seed, residual}: y = (residual +) (kept ? x / (1 - rate) : 0), x and residual of one
+                                 shape. seed [1][1][1][2]: the bit patterns of its two values (any 64 bits: two floats that count steps as
+                                 well as two words) are the key; another seed is another mask, the same seed the same one, which is not
+                                 stored: THE GRADIENT is this operator on {dy, seed} with the same rate and site. Element e (counted in memory
+                                 order) is kept if word e % 4 of Philox4x32-10 with counter (low, high word of e / 4, site, 0) is at least
+                                 L = round(rate 2^32); 1 / (1 - rate) is 2^32 / (2^32 - L). 0 <= rate < 1 (0: every element is kept). Dropped
+                                 infinities and NaN are dropped like other values */
+    NG_OP_POSITION_BIAS = 37, /* no preds, weights {table[buckets][heads]} -> [1][heads][1][2 m + 1], m = max_distance: the attention bias of a
+                                 key at distance d = -m .. m from its query, table[bucket(d)][head]. With both != 0, b = buckets / 2 (buckets
+                                 even) and keys behind the query (d > 0) have the buckets from b on; with both = 0, b = buckets and keys behind
+                                 the query are not seen: -infinity. e = b / 2 >= 1, e < m <= 1023:
+                                   bucket(d) = |d| for |d| < e, else min(b - 1, e + floor((b - e) log(|d| / e) / log(m / e)))
+                                 (in 64 bits; a border counts as reached from 1e-9 below it on) */
+    NG_OP_POSITION_BIAS_WGRAD = 38 /* preds {gradient of the bias, [1][heads][1][2 m + 1]}, no weights, same parameters -> dtable as
+                                 [buckets][heads][1][1] */
 };
 
 typedef struct ng_op_params {
@@ -128,16 +149,21 @@ typedef struct ng_op_params {
     int32_t pad;       /* CONV3X3, POOL: 0 or 1 */
     int32_t relu;      /* BN_ACT */
     int32_t pool_mode; /* POOL: 0 max, 1 avg */
-    float eps;         /* BN_ACT, HEAD_ROPE* */
+    float eps;         /* BN_ACT, HEAD_ROPE*, LAYER_NORM* */
     int32_t slice_lo[NG_MAX_PREDS]; /* CONCAT; slice_hi[j] == 0 means "all channels of pred j" */
     int32_t slice_hi[NG_MAX_PREDS];
     float lr;          /* SGD_UPDATE */
-    int32_t heads;     /* HEAD_ROPE*, ATTENTION*: heads of x, of q */
+    int32_t heads;     /* HEAD_ROPE*, ATTENTION*, POSITION_BIAS*: heads of x, of q */
     int32_t kv_heads;  /* ATTENTION, _DQ, _DK, _DV: heads of k and v */
     int32_t rot;       /* HEAD_ROPE*: channels of a head that are rotated */
     int32_t interleaved; /* HEAD_ROPE*: which channels are a pair */
     float factor;      /* HEAD_ROPE*: on the rotated channels (1: a rotation; scaled long contexts may want another), not 0 */
     float scale;       /* ATTENTION, _DQ, _DK, _DV: on the scores, not 0 */
+    float rate;        /* DROPOUT: share of the elements that is dropped, 0 <= rate < 1 */
+    int32_t site;      /* DROPOUT: >= 0; nodes with different sites have different masks under one seed */
+    int32_t buckets;   /* POSITION_BIAS*: rows of the table */
+    int32_t max_distance; /* POSITION_BIAS*: from here on distances have the last bucket; at most 1023 */
+    int32_t both;      /* POSITION_BIAS*: keys behind the query have buckets of their own (0: they are not seen) */
 } ng_op_params;
 
 typedef struct ng_graph ng_graph; /* opaque */
@@ -154,7 +180,7 @@ void ng_destroy(ng_graph* g);
 int ng_add_input(ng_graph* g, const int64_t nchw[4], int* id);
 
 /* Add an operator node. preds (host array of n_preds ids) must name existing nodes, so
- * ids are a topological order of the DAG. dev_weights (host array of n_weights DEVICE
+ * ids are a topological order of the DAG (one of them at least, but for NG_OP_POSITION_BIAS, which reads weights only). dev_weights (host array of n_weights DEVICE
  * pointers, caller-owned) are the operator's parameters in the order listed at the op
  * enum; they may be NULL pointers until ng_capture (host-only use). The output shape is
  * inferred here; a mismatch returns NG_ESHAPE and leaves the graph unchanged. */
@@ -239,7 +265,7 @@ int ng_set_memory_reuse(ng_graph* g, int on);
  * and x) are computed in one walk over dy and x by the launch of whichever of the two comes first, if
  * both are on one stream (always, in modes 1 and 2); likewise the input gradient and the weight gradient
  * of a depthwise or 1 x 1 convolution (same dy) share one launch, their workgroups interleaved, if
- * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, and dk and
+ * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, those of NG_OP_LAYER_NORM, and dk and
  * dv of an attention with many keys and heads of up to 64 channels, with what both need computed once. In modes 1 and 2 tasks of the
  * same kernel that do not wait for each other share a launch as well, and the launches follow each other in an
  * order that lets them (ng_get_single_launches; attention operators' kernels have a launch each). on = 0 switches the exceptions off: one kernel per task. Call before ng_bind (NG_ESTATE after). */

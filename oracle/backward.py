@@ -30,7 +30,7 @@ from typing import Dict, List, Optional, Tuple
 import numpy as np
 
 from . import ops
-from .forward import eval_node, input_value
+from .forward import attention_extras, eval_node, input_value
 
 
 def _f64(x):
@@ -135,14 +135,17 @@ def head_rope_vjp(x, positions, freq, gamma, heads, interleaved, eps, factor, dy
     return dx.reshape(n, c, h, w), (du * xh).sum(axis=(0, 1, 3))
 
 
-def attention_vjp(q, k, v, lengths, heads, kv_heads, scale, dy):
-    """dv = p^T dy; ds = p (dp - <p, dp>) with dp = <dy, v>; dq = scale ds k, dk = scale ds^T q; heads that share a key head add up."""
-    p = ops.attention_weights(q, k, heads, kv_heads, scale, lengths)
+def attention_vjp(q, k, v, lengths, heads, kv_heads, scale, dy, bias=None, at="first"):
+    """dv = p^T dy; ds = p (dp - <p, dp>) with dp = <dy, v>; dq = scale ds k, dk = scale ds^T q; heads that share a key head add up.
+    With a bias (dq, dk, dv, dbias): dbias[head][distance] = the sum of ds over all pairs at that distance."""
+    p = ops.attention_weights(q, k, heads, kv_heads, scale, lengths, bias, at)
     n, group = p.shape[0], heads // kv_heads
     qh, gh = (_f64(t).reshape(n, heads, -1, p.shape[2]) for t in (q, dy))
     kh, vh = (ops.counted_values(t, kv_heads, lengths) for t in (k, v))
     dq, dk, dv = np.zeros_like(qh), np.zeros_like(kh), np.zeros_like(vh)
+    dbias = None if bias is None else np.zeros((heads, np.size(bias) // heads))
     for b in range(n):
+        m = p.shape[3] if lengths is None else ops.key_count(float(np.ravel(lengths)[b]), p.shape[3])
         for h in range(heads):
             j = h // group
             dv[b, j] += gh[b, h] @ p[b, h]
@@ -150,7 +153,31 @@ def attention_vjp(q, k, v, lengths, heads, kv_heads, scale, dy):
             ds = p[b, h] * (dp - (p[b, h] * dp).sum(axis=1, keepdims=True))
             dq[b, h] = scale * (kh[b, j] @ ds.T)
             dk[b, j] += scale * (qh[b, h] @ ds)
-    return dq.reshape(np.shape(q)), dk.reshape(np.shape(k)), dv.reshape(np.shape(v))
+            if bias is not None:
+                place = ops.distances(p.shape[2], m, dbias.shape[1] // 2, m - p.shape[2] if at == "last" else 0)
+                np.add.at(dbias[h], place, ds[:, :m])
+    out = dq.reshape(np.shape(q)), dk.reshape(np.shape(k)), dv.reshape(np.shape(v))
+    return out if bias is None else out + (dbias.reshape(np.shape(bias)),)
+
+
+def layer_norm_vjp(x, gamma, eps, dy):
+    """With xh the normed x and u = gamma dy: dx = (u - mean u - xh mean(u xh)) / sqrt(variance + eps); dgamma = sum dy xh, dbeta = sum dy."""
+    x, dy = _f64(x), _f64(dy)
+    centred = x - x.mean(axis=1, keepdims=True)
+    sd = np.sqrt((centred * centred).mean(axis=1, keepdims=True) + eps)
+    xh, u = centred / sd, dy * _f64(gamma)[None, :, None, None]
+    dx = (u - u.mean(axis=1, keepdims=True) - xh * (u * xh).mean(axis=1, keepdims=True)) / sd
+    return dx, (dy * xh).sum(axis=(0, 2, 3)), dy.sum(axis=(0, 2, 3))
+
+
+def position_bias_vjp(dbias, heads, buckets, max_distance, both):
+    dbias = _f64(dbias).reshape(heads, -1)
+    dtable = np.zeros((buckets, heads))
+    for d in range(-max_distance, max_distance + 1):
+        b = ops.position_bucket(d, buckets, max_distance, both)
+        if b is not None:
+            dtable[b] += dbias[:, d + max_distance]
+    return dtable
 
 
 def node_vjp(nd, ins, dy) -> Tuple[List[np.ndarray], List[np.ndarray]]:
@@ -192,9 +219,17 @@ def node_vjp(nd, ins, dy) -> Tuple[List[np.ndarray], List[np.ndarray]]:
         dx, dg = head_rope_vjp(ins[0], ins[1], w[0], w[1] if len(w) > 1 else None, p["heads"], bool(p["interleaved"]), p["eps"], p["factor"], dy)
         return [dx, np.zeros(ins[1].shape)], [np.zeros(len(w[0]))] + ([dg] if dg is not None else [])
     if nd.op == "attention":
-        lengths = ins[3] if len(ins) > 3 else None
-        grads = attention_vjp(ins[0], ins[1], ins[2], lengths, p["heads"], p["kv_heads"], p["scale"], dy)
-        return list(grads) + ([np.zeros(lengths.shape)] if lengths is not None else []), []
+        lengths, bias = attention_extras(nd, ins)
+        grads = list(attention_vjp(ins[0], ins[1], ins[2], lengths, p["heads"], p["kv_heads"], p["scale"], dy, bias, p.get("bias", "first")))
+        return grads[:3] + ([np.zeros(lengths.shape)] if lengths is not None else []) + grads[3:], []
+    if nd.op == "layer_norm":
+        dx, dg, db = layer_norm_vjp(ins[0], w[0], p["eps"], dy)
+        return [dx], [dg, db]
+    if nd.op == "dropout":
+        m = ops.dropout_scale(np.shape(ins[0]), ins[1], p["rate"], p["site"])
+        return [_f64(dy) * m, np.zeros(ins[1].shape)] + ([_f64(dy).copy()] if len(ins) > 2 else []), []
+    if nd.op == "position_bias":
+        return [], [position_bias_vjp(dy, p["heads"], p["buckets"], p["max_distance"], bool(p["both"]))]
     raise ValueError(f"unknown op {nd.op!r}")
 
 

@@ -38,8 +38,22 @@ def eval_node(nd, ins):
     if nd.op == "head_rope":
         return ops.head_rope(ins[0], ins[1], w[0], w[1] if len(w) > 1 else None, p["heads"], bool(p["interleaved"]), p["eps"], p["factor"])
     if nd.op == "attention":
-        return ops.attention(ins[0], ins[1], ins[2], ins[3] if len(ins) > 3 else None, p["heads"], p["kv_heads"], p["scale"])
+        lengths, bias = attention_extras(nd, ins)
+        return ops.attention(ins[0], ins[1], ins[2], lengths, p["heads"], p["kv_heads"], p["scale"], bias, p.get("bias", "first"))
+    if nd.op == "layer_norm":
+        return ops.layer_norm(ins[0], w[0], w[1], p["eps"])
+    if nd.op == "dropout":
+        return ops.dropout(ins[0], ins[1], ins[2] if len(ins) > 2 else None, p["rate"], p["site"])
+    if nd.op == "position_bias":
+        return ops.position_bias(w[0], p["heads"], p["buckets"], p["max_distance"], bool(p["both"]))
     raise ValueError(f"unknown op {nd.op!r}")
+
+
+def attention_extras(nd, ins):
+    """Lengths and bias of an attention node, None where it has none."""
+    rest = list(ins[3:])
+    bias = rest.pop() if "bias" in nd.params else None
+    return (rest[0] if rest else None), bias
 
 
 def input_value(workload, v, x):

@@ -164,18 +164,32 @@ def key_count(length, tk: int) -> int:
     return sum(1 for j in range(tk) if j < length)
 
 
-def attention_weights(q, k, heads: int, kv_heads: int, scale: float, lengths):
-    """p[n][head][query][key]: softmax over the keys that count, 0 for the others (and everywhere for an image without any)."""
+def distances(tq: int, tk: int, reach: int, offset: int):
+    """[query][key]: place of the distance j - (i + offset) in a bias of the distances -reach .. reach; farther ones are taken as these."""
+    d = np.arange(tk)[None, :] - (np.arange(tq)[:, None] + offset)
+    return np.clip(d, -reach, reach) + reach
+
+
+def attention_weights(q, k, heads: int, kv_heads: int, scale: float, lengths, bias=None, at: str = "first"):
+    """p[n][head][query][key]: softmax over the keys that count (and, with a bias, are seen: not -infinity), 0 for the others (and everywhere
+    for a query without any). ``at``: the bias counts distances from the first key ("first") or so that the last query is at the last
+    key that counts ("last")."""
     q, k = _f64(q), _f64(k)
     n, c = q.shape[:2]
     q, k = q.reshape(n, heads, c // heads, -1), k.reshape(n, kv_heads, c // heads, -1)
-    p = np.zeros((n, heads, q.shape[3], k.shape[3]))
+    tq, tk = q.shape[3], k.shape[3]
+    p = np.zeros((n, heads, tq, tk))
     for b in range(n):
-        m = k.shape[3] if lengths is None else key_count(float(np.ravel(lengths)[b]), k.shape[3])
+        m = tk if lengths is None else key_count(float(np.ravel(lengths)[b]), tk)
         for h in range(heads if m else 0):
             s = scale * (q[b, h].T @ k[b, h // (heads // kv_heads)][:, :m])
-            e = np.exp(s - s.max(axis=1, keepdims=True))
-            p[b, h, :, :m] = e / e.sum(axis=1, keepdims=True)
+            if bias is not None:
+                row = _f64(bias).reshape(heads, -1)[h]
+                s = s + row[distances(tq, m, len(row) // 2, m - tq if at == "last" else 0)]
+            top = s.max(axis=1, keepdims=True)
+            e = np.exp(s - np.where(np.isneginf(top), 0.0, top))
+            total = e.sum(axis=1, keepdims=True)
+            p[b, h, :, :m] = e / np.where(total == 0.0, 1.0, total)
     return p
 
 
@@ -188,9 +202,67 @@ def counted_values(v, kv_heads: int, lengths):
     return v
 
 
-def attention(q, k, v, lengths, heads: int, kv_heads: int, scale: float):
+def attention(q, k, v, lengths, heads: int, kv_heads: int, scale: float, bias=None, at: str = "first"):
     """y[query] = sum over keys p[query][key] v[key]."""
-    p = attention_weights(q, k, heads, kv_heads, scale, lengths)
+    p = attention_weights(q, k, heads, kv_heads, scale, lengths, bias, at)
     vh = counted_values(v, kv_heads, lengths)
     y = np.stack([np.stack([vh[b, h // (heads // kv_heads)] @ p[b, h].T for h in range(heads)]) for b in range(p.shape[0])])
     return _out(y.reshape(q.shape))
+
+
+def layer_norm(x, gamma, beta, eps: float):
+    """gamma (x - mean) / sqrt(variance + eps) + beta over the channels of each pixel."""
+    x = _f64(x)
+    centred = x - x.mean(axis=1, keepdims=True)
+    xh = centred / np.sqrt((centred * centred).mean(axis=1, keepdims=True) + eps)
+    return _out(xh * _f64(gamma)[None, :, None, None] + _f64(beta)[None, :, None, None])
+
+
+def philox4x32(counter, key):
+    """Ten rounds of Philox4x32 (Salmon et al., SC 2011) on counters [m][4] with a key of two words: [m][4] words."""
+    c = [counter[:, j].astype(np.uint64) for j in range(4)]
+    k = [int(key[0]), int(key[1])]
+    low = np.uint64(0xFFFFFFFF)
+    for _ in range(10):
+        a, b = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(b >> np.uint64(32)) ^ c[1] ^ np.uint64(k[0]), b & low, (a >> np.uint64(32)) ^ c[3] ^ np.uint64(k[1]), a & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return np.stack(c, 1).astype(np.uint32)
+
+
+def dropout_scale(shape, seed, rate: float, site: int):
+    """What each element is multiplied by: 1 / (1 - rate) where it is kept, 0 where it is dropped (rate rounded to 2^-32)."""
+    total = int(np.prod(shape))
+    e = np.arange((total + 3) // 4, dtype=np.uint64)
+    counter = np.stack([e & np.uint64(0xFFFFFFFF), e >> np.uint64(32), np.full_like(e, site), np.zeros_like(e)], 1)
+    words = philox4x32(counter, np.ascontiguousarray(seed, dtype=np.float32).reshape(2).view(np.uint32)).ravel()[:total]
+    limit = int(np.rint(float(np.float32(rate)) * 2.0 ** 32))
+    return np.where(words.astype(np.int64) >= limit, 2.0 ** 32 / (2.0 ** 32 - limit), 0.0).reshape(shape)
+
+
+def dropout(x, seed, residual, rate: float, site: int):
+    m = dropout_scale(np.shape(x), seed, rate, site)
+    y = np.where(m > 0, _f64(x) * m, 0.0) if m.size else m
+    return _out(y if residual is None else _f64(residual) + y)
+
+
+def position_bucket(distance: int, buckets: int, max_distance: int, both: bool):
+    """Bucket of a distance (key less query), None for keys behind the query where they are not seen. In whole numbers: step j of the
+    logarithmic buckets is reached where (|d| / exact)^steps >= (max_distance / exact)^j."""
+    b = buckets // 2 if both else buckets
+    exact, far = b // 2, abs(distance)
+    if distance > 0 and not both:
+        return None
+    if far >= exact:
+        steps = b - exact
+        j = 0
+        while j < steps and far ** steps * exact ** (j + 1) >= max_distance ** (j + 1) * exact ** steps:
+            j += 1
+        far = min(exact + j, b - 1)
+    return far + (b if distance > 0 else 0)
+
+
+def position_bias(table, heads: int, buckets: int, max_distance: int, both: bool):
+    table = _f64(table).reshape(buckets, heads)
+    of = [position_bucket(d, buckets, max_distance, both) for d in range(-max_distance, max_distance + 1)]
+    return _out(np.stack([np.full(heads, -np.inf) if b is None else table[b] for b in of], 1).reshape(1, heads, 1, -1))

@@ -54,15 +54,26 @@ enum Kid : int {
     KID_ATTN_ROWS,
     // a wavefront owns 16 queries (DK, DV: 16 keys) of heads of up to 64 / 128 channels and reads its operands straight from memory
     KID_ATTN_W64, KID_ATTN_W128, KID_ATTN_DQ_W64, KID_ATTN_DQ_W128, KID_ATTN_DK_W64, KID_ATTN_DK_W128, KID_ATTN_DV_W64, KID_ATTN_DV_W128,
+    // layer norm: a thread has four tokens (V) or one (S) and up to 8 or 16 channels in registers
+    KID_NORM_V8, KID_NORM_V16, KID_NORM_S16,
+    KID_DROPOUT, KID_POSITION_BIAS, KID_POSITION_BIAS_WGRAD,
     // the same for many columns: 128 for each workgroup, the other side staged through LDS (launched kernels only)
     KID_ATTN_T64, KID_ATTN_T128, KID_ATTN_DQ_T64, KID_ATTN_DQ_T128, KID_ATTN_DK_T64, KID_ATTN_DK_T128, KID_ATTN_DV_T64, KID_ATTN_DV_T128, KID_ATTN_DKV_T64,
     // both gradients of norm and rotation in one launch (launched kernels only)
     KID_ROPE_BOTH_4, KID_ROPE_BOTH_8, KID_ROPE_BOTH_N,
+    // layer norm, launched kernels only (the resident kernel with these took 366 s to compile instead of 165): any number of channels,
+    // which come from memory again for each sum (M); workgroups of 1024 threads for many channels (W); dx, the gradients of gamma and
+    // beta, and all of them in one launch
+    KID_NORM_M, KID_NORM_W16,
+    KID_NORM_DX_V8, KID_NORM_DX_V16, KID_NORM_DX_S16, KID_NORM_DX_M, KID_NORM_DX_W16,
+    KID_NORM_DG_V8, KID_NORM_DG_V16, KID_NORM_DG_S16, KID_NORM_DG_M, KID_NORM_DG_W16,
+    KID_NORM_BOTH_V8, KID_NORM_BOTH_V16, KID_NORM_BOTH_S16, KID_NORM_BOTH_M, KID_NORM_BOTH_W16,
     KID_COUNT
 };
 constexpr bool is_attention_tile_kernel(int kid) { return kid >= KID_ATTN_T64 && kid <= KID_ATTN_DKV_T64; }
 constexpr bool is_launched_attention_kernel(int kid) { return kid >= KID_ATTN_T64 && kid < KID_COUNT; }
 constexpr bool is_attention_kernel(int kid) { return kid >= KID_ROPE_4 && kid < KID_COUNT; }
+constexpr bool is_wide_norm(int kid) { return kid == KID_NORM_W16 || kid == KID_NORM_DX_W16 || kid == KID_NORM_DG_W16 || kid == KID_NORM_BOTH_W16; }
 constexpr bool is_train_kernel(int kid) { return kid >= KID_GEMM_PW_FWD && kid <= KID_SGD; }
 
 // the variant without / with a fused add_n of a kernel (ids without such a variant map to themselves / KID_NONE)
@@ -141,6 +152,7 @@ constexpr bool in_build(int build, int kid) {
 }
 
 constexpr int kBlock = 256;          // threads that work on one tile (a stand-alone kernel's workgroup)
+constexpr int block_threads(int kid) { return is_wide_norm(kid) ? 1024 : kBlock; }      // (kernels that are only launched may have more)
 constexpr int kSubs = 2;             // tiles a workgroup of the resident kernel works on at a time
 constexpr int kGroup = kBlock * kSubs;  // threads per workgroup of the resident kernel
 constexpr int kArgBytes = 256;       // size of the per-task argument block of the resident kernel's task table
@@ -397,6 +409,7 @@ struct SgdBatchArgs {
 
 // ---- attention ---------------------------------------------------------------------------
 constexpr int kRopeMaxHead = 256, kAttentionMaxHead = 128;   // channels of a head
+constexpr int kMaxReach = 1023;                              // distances told apart by a bias, to each side
 struct RopeArgs {
     const float* x;            // [n][heads d][T]
     const float* dy;           // gradients: of the result
@@ -428,6 +441,39 @@ struct AttnArgs {
     int N, H, Hk, d, Tq, Tk;
     int col_blocks;            // blocks of columns (queries of the heads that share a key head; dk, dv: keys) for each image and key head
     int splits, per_split;     // the other side (keys; dk, dv: queries) is cut into splits of per_split blocks
+};
+
+// ---- around the attention of a block --------------------------------------------------------
+struct NormArgs {
+    const float* x;            // [n][C][T]
+    const float* dy;           // gradients: of the result
+    const float* gamma; const float* beta;
+    float* y;                  // forward: y; dgrad: dx
+    float* ws;                 // wgrad: sums of each workgroup [tiles][2 C], then of each group of workgroups
+    unsigned* cnt;             // wgrad: arrivals, zero between replays
+    float* dg;                 // wgrad: dgamma [C], dbeta [C]
+    float eps;
+    int C, T;
+    int lanes_log2;            // threads of a workgroup that are side by side along the tokens
+    int blocks;                // blocks of tokens of an image
+    int items, per_tile;       // blocks of all images, and how many of them a workgroup walks
+    int tiles;
+};
+struct DropoutArgs {
+    const float* x;
+    const float* seed;         // two words
+    const float* residual;     // or nullptr
+    float* y;
+    long total;
+    unsigned site, limit;      // an element is dropped if its random word is below the limit
+    float scale;
+};
+struct PositionBiasArgs {
+    const float* table;        // forward: [buckets][heads]
+    const float* dbias;        // wgrad: [heads][distances]
+    const int* bucket_of;      // [distances], -1: not seen
+    float* out;
+    int heads, distances, buckets;
 };
 
 // Two tasks in one launch: tiles of both, dealt out alternately while both have tiles left (depthwise; conv1x1: pw_backward_share).

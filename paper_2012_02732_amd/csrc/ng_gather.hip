@@ -64,7 +64,8 @@ __global__ __launch_bounds__(kBlock, min_waves(KID)) void timed_gathered_kernel(
     X(KID_C3_M1) X(KID_C3_M2) X(KID_C3_M3) X(KID_C3_M4) X(KID_C3_L32) X(KID_C3_L64)                                     \
     X(KID_C3_P64) X(KID_C3_P96) X(KID_C3_Q32) X(KID_C3_Q64) X(KID_C3_Q128) X(KID_C3_R32) X(KID_C3_R128) X(KID_C3_SK)     \
     X(KID_PW_PX_FWD) X(KID_BN_RAW) X(KID_BN_BACKWARD) X(KID_PAIR_DW) X(KID_PAIR_DW_LDS) X(KID_PAIR_PW16)                \
-    X(KID_PAIR_PW32) X(KID_POOL_DGRAD) X(KID_POOL_DGRAD_LDS) X(KID_SLICE_PAD) X(KID_SMALL_GEMM)
+    X(KID_PAIR_PW32) X(KID_POOL_DGRAD) X(KID_POOL_DGRAD_LDS) X(KID_SLICE_PAD) X(KID_SMALL_GEMM)  \
+    X(KID_DROPOUT)
 
 // conv1x1 from this many column blocks on: they are dealt out to the XCDs (xcd_share). In the tiles' own order the row tiles of a
 // column block run on up to 8 XCDs and each of those reads the block into its own L2. Dealt out, the launches of 64 x 64 tiles of the
@@ -124,7 +125,7 @@ void make_gathered_launch(const std::vector<const Task*>& tasks, SingleLaunch& o
         if (t->kid != tasks[0]->kid || !t->fn) return;
     if (tasks.size() == 1) {
         const Task& t = *tasks[0];
-        out.fn = t.fn, out.timed_fn = timed_kernel_handle(t.kid), out.grid = t.grid[0], out.lds_bytes = t.lds_bytes;
+        out.fn = t.fn, out.timed_fn = timed_kernel_handle(t.kid), out.grid = t.grid[0], out.block = t.block[0], out.lds_bytes = t.lds_bytes;
         out.args.assign(t.args, t.args + sizeof t.args);
         if (!is_pw_columns(t.kid)) return;
     }

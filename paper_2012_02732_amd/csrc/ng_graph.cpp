@@ -288,6 +288,42 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
             out.c = 3 * p.heads;
             return nullptr;
         }
+        case NG_OP_LAYER_NORM:
+        case NG_OP_LAYER_NORM_DGRAD:
+        case NG_OP_LAYER_NORM_WGRAD: {
+            const bool backward = op != NG_OP_LAYER_NORM;
+            if (!need(backward ? 2 : 1, 2)) return backward ? "layer_norm backward takes dy and x, and gamma and beta of the forward operator" : "layer_norm takes x, and gamma and beta";
+            if (!(p.eps >= 0.f) || !std::isfinite(p.eps)) return "layer_norm: eps must be >= 0 and finite";
+            const Shape& x = in(backward ? 1 : 0);
+            code = NG_ESHAPE;
+            if (backward && !(in(0) == x)) return "layer_norm backward: dy and x differ in shape";
+            if (x.c * x.h * x.w > kMaxSliceElems) return "layer_norm: an image has more than 2^29 values";
+            out = op == NG_OP_LAYER_NORM_WGRAD ? Shape{2, x.c, 1, 1} : x;
+            return nullptr;
+        }
+        case NG_OP_DROPOUT:
+            if ((n_preds != 2 && n_preds != 3) || n_weights != 0) return "dropout takes x, the seed and, if wanted, a residual";
+            if (!(p.rate >= 0.f) || !(p.rate < 1.f)) return "dropout: rate must be at least 0 and below 1";
+            if (p.site < 0) return "dropout: site must be at least 0";
+            code = NG_ESHAPE;
+            if (!(in(1) == Shape{1, 1, 1, 2})) return "dropout: the seed must be [1][1][1][2]";
+            if (n_preds == 3 && !(in(2) == in(0))) return "dropout: x and the residual differ in shape";
+            out = in(0);
+            return nullptr;
+        case NG_OP_POSITION_BIAS:
+        case NG_OP_POSITION_BIAS_WGRAD: {
+            const bool wgrad = op == NG_OP_POSITION_BIAS_WGRAD;
+            if (!need(wgrad ? 1 : 0, wgrad ? 0 : 1)) return wgrad ? "position_bias_wgrad takes the gradient of the bias" : "position_bias takes no inputs and 1 weight (the table)";
+            if (p.heads <= 0 || p.heads > (1 << 20)) return "position_bias: heads must be positive and at most 2^20";
+            if (!in_set(p.both, 0, 1)) return "position_bias: both in {0,1}";
+            if (p.buckets < (p.both ? 4 : 2) || p.buckets > (1 << 20) || (p.both && p.buckets % 2 != 0)) return "position_bias: buckets must be at least 2, or even and at least 4 for both directions, and at most 2^20";
+            if (p.max_distance > kMaxReach || p.max_distance <= (p.both ? p.buckets / 2 : p.buckets) / 2) return "position_bias: max_distance must be more than half of a direction's buckets and at most 1023";
+            const Shape bias{1, p.heads, 1, 2 * (int64_t)p.max_distance + 1};
+            code = NG_ESHAPE;
+            if (wgrad && !(in(0) == bias)) return "position_bias_wgrad: the gradient must be [1][heads][1][2 max_distance + 1]";
+            out = wgrad ? Shape{p.buckets, p.heads, 1, 1} : bias;
+            return nullptr;
+        }
         default:
             return "unknown operator kind";
     }
@@ -339,7 +375,7 @@ int ng_add_node(ng_graph* g, int op_kind, const ng_op_params* p, const int* pred
         return g->fail(NG_EINVAL, "ng_add_node: null or negative argument");
     if (g->phase != BUILDING) return g->fail(NG_ESTATE, "ng_add_node: registration is closed");
     if (op_kind == NG_OP_INPUT) return g->fail(NG_EINVAL, "ng_add_node: use ng_add_input for inputs");
-    if (n_preds == 0 || n_preds > NG_MAX_PREDS) return g->fail(NG_EINVAL, "ng_add_node: needs 1..%d predecessors", NG_MAX_PREDS);
+    if ((n_preds == 0 && op_kind != NG_OP_POSITION_BIAS) || n_preds > NG_MAX_PREDS) return g->fail(NG_EINVAL, "ng_add_node: needs 1..%d predecessors", NG_MAX_PREDS);
     for (int j = 0; j < n_preds; ++j)
         if (preds[j] < 0 || preds[j] >= (int)g->nodes.size())
             return g->fail(NG_EINVAL, "ng_add_node: predecessor id %d does not exist", preds[j]);
@@ -351,8 +387,8 @@ int ng_add_node(ng_graph* g, int op_kind, const ng_op_params* p, const int* pred
         return g->fail(code, "ng_add_node(node %d): %s", (int)g->nodes.size(), msg);
     if (nd.out.elems() <= 0 || nd.out.elems() >= ((int64_t)1 << 31))
         return g->fail(NG_ESHAPE, "ng_add_node: tensor of %lld elements is not supported", (long long)nd.out.elems());
-    nd.preds.assign(preds, preds + n_preds);
-    nd.weights.assign(dev_weights, dev_weights + n_weights);
+    if (n_preds > 0) nd.preds.assign(preds, preds + n_preds);
+    if (n_weights > 0) nd.weights.assign(dev_weights, dev_weights + n_weights);
     g->nodes.push_back(std::move(nd));
     *id = (int)g->nodes.size() - 1;
     return NG_OK;
@@ -636,6 +672,12 @@ int ng_task_work(const ng_graph* g, int id, double* bytes, double* flops) {
             break;
         }
         case NG_OP_ATTENTION_ROWS: b = 4 * (2 * in0 + out), f = 2 * in0; break;
+        case NG_OP_LAYER_NORM: b = 4 * (2 * out + 2.0 * nd.out.c), f = 8 * out; break;
+        case NG_OP_LAYER_NORM_DGRAD: b = 4 * (3 * out + 2.0 * nd.out.c), f = 14 * out; break;
+        case NG_OP_LAYER_NORM_WGRAD: b = 4 * (2 * in0 + out), f = 8 * in0; break;
+        case NG_OP_DROPOUT: b = 4 * ((double)nd.preds.size() * out + 2), f = 25 * out; break;      // (integer operations of the generator: a round's for four elements)
+        case NG_OP_POSITION_BIAS: b = 4 * (out + (double)nd.p.buckets * nd.p.heads), f = 0; break;
+        case NG_OP_POSITION_BIAS_WGRAD: b = 4 * (in0 + out), f = in0; break;
         case NG_OP_SGD_UPDATE: b = 12.0 * nd.p.cout; f = 2.0 * nd.p.cout; break;
         default: break;
     }

@@ -96,7 +96,7 @@ struct ResidentPlan {
 struct SingleLaunch {
     const void* fn = nullptr;
     const void* timed_fn = nullptr;            // the same with the device's clock read around every workgroup
-    unsigned grid = 0, lds_bytes = 0;
+    unsigned grid = 0, block = kBlock, lds_bytes = 0;
     std::vector<unsigned char> args;
 };
 

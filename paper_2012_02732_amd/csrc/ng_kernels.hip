@@ -1832,6 +1832,7 @@ __device__ __forceinline__ void dwconv_lds_tile(const DwArgs& a, int tile, float
 
 #include "ng_train_tiles.inc"
 #include "ng_attention_tiles.inc"
+#include "ng_block_tiles.inc"
 
 // ------------------------------------------------------------------------------------
 // kernel table: id -> argument type, tile function, name
@@ -2030,8 +2031,31 @@ NG_KERNEL(KID_ATTN_DKV_T64, PairAttnArgs, "attention_dk+dv_tile_64", attention_d
 NG_KERNEL(KID_ROPE_BOTH_4, RopeArgs, "head_rope_dgrad+wgrad_128", rope_tile < ROPE_BOTH, 4)
 NG_KERNEL(KID_ROPE_BOTH_8, RopeArgs, "head_rope_dgrad+wgrad_256", rope_tile < ROPE_BOTH, 8)
 NG_KERNEL(KID_ROPE_BOTH_N, RopeArgs, "head_rope_dgrad+wgrad_few", rope_few_tile < ROPE_BOTH)
+NG_KERNEL(KID_NORM_V8, NormArgs, "layer_norm_8", norm_tile < NORM_FWD, 256, 4, 8)
+NG_KERNEL(KID_NORM_V16, NormArgs, "layer_norm_16", norm_tile < NORM_FWD, 256, 4, 16)
+NG_KERNEL(KID_NORM_S16, NormArgs, "layer_norm_few", norm_tile < NORM_FWD, 256, 1, 16)
+NG_KERNEL(KID_NORM_M, NormArgs, "layer_norm_many", norm_many_tile < NORM_FWD)
+NG_KERNEL(KID_NORM_W16, NormArgs, "layer_norm_wide", norm_tile < NORM_FWD, 1024, 4, 16)
+NG_KERNEL(KID_NORM_DX_V8, NormArgs, "layer_norm_dgrad_8", norm_tile < NORM_DX, 256, 4, 8)
+NG_KERNEL(KID_NORM_DX_V16, NormArgs, "layer_norm_dgrad_16", norm_tile < NORM_DX, 256, 4, 16)
+NG_KERNEL(KID_NORM_DX_S16, NormArgs, "layer_norm_dgrad_few", norm_tile < NORM_DX, 256, 1, 16)
+NG_KERNEL(KID_NORM_DX_M, NormArgs, "layer_norm_dgrad_many", norm_many_tile < NORM_DX)
+NG_KERNEL(KID_NORM_DX_W16, NormArgs, "layer_norm_dgrad_wide", norm_tile < NORM_DX, 1024, 4, 16)
+NG_KERNEL(KID_NORM_DG_V8, NormArgs, "layer_norm_wgrad_8", norm_tile < NORM_DG, 256, 4, 8)
+NG_KERNEL(KID_NORM_DG_V16, NormArgs, "layer_norm_wgrad_16", norm_tile < NORM_DG, 256, 4, 16)
+NG_KERNEL(KID_NORM_DG_S16, NormArgs, "layer_norm_wgrad_few", norm_tile < NORM_DG, 256, 1, 16)
+NG_KERNEL(KID_NORM_DG_M, NormArgs, "layer_norm_wgrad_many", norm_many_tile < NORM_DG)
+NG_KERNEL(KID_NORM_DG_W16, NormArgs, "layer_norm_wgrad_wide", norm_tile < NORM_DG, 1024, 4, 16)
+NG_KERNEL(KID_NORM_BOTH_V8, NormArgs, "layer_norm_dgrad+wgrad_8", norm_tile < NORM_BOTH, 256, 4, 8)
+NG_KERNEL(KID_NORM_BOTH_V16, NormArgs, "layer_norm_dgrad+wgrad_16", norm_tile < NORM_BOTH, 256, 4, 16)
+NG_KERNEL(KID_NORM_BOTH_S16, NormArgs, "layer_norm_dgrad+wgrad_few", norm_tile < NORM_BOTH, 256, 1, 16)
+NG_KERNEL(KID_NORM_BOTH_M, NormArgs, "layer_norm_dgrad+wgrad_many", norm_many_tile < NORM_BOTH)
+NG_KERNEL(KID_NORM_BOTH_W16, NormArgs, "layer_norm_dgrad+wgrad_wide", norm_tile < NORM_BOTH, 1024, 4, 16)
 #undef NG_KERNEL
 NG_KERNEL0(KID_ATTN_ROWS, AttnArgs, "attention_rows", attention_rows_tile)
+NG_KERNEL0(KID_DROPOUT, DropoutArgs, "dropout", dropout_tile)
+NG_KERNEL0(KID_POSITION_BIAS, PositionBiasArgs, "position_bias", position_bias_tile)
+NG_KERNEL0(KID_POSITION_BIAS_WGRAD, PositionBiasArgs, "position_bias_wgrad", position_bias_wgrad_tile)
 NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
 #undef NG_KERNEL0
 
@@ -2056,7 +2080,12 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_ATTN_ROWS) X(KID_ATTN_W64) X(KID_ATTN_W128) X(KID_ATTN_DQ_W64) X(KID_ATTN_DQ_W128) X(KID_ATTN_DK_W64) X(KID_ATTN_DK_W128)    \
     X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128) X(KID_ATTN_T64) X(KID_ATTN_T128) X(KID_ATTN_DQ_T64) X(KID_ATTN_DQ_T128)    \
     X(KID_ATTN_DK_T64) X(KID_ATTN_DK_T128) X(KID_ATTN_DV_T64) X(KID_ATTN_DV_T128)    \
-    X(KID_ATTN_DKV_T64) X(KID_ROPE_BOTH_4) X(KID_ROPE_BOTH_8) X(KID_ROPE_BOTH_N)
+    X(KID_ATTN_DKV_T64) X(KID_ROPE_BOTH_4) X(KID_ROPE_BOTH_8) X(KID_ROPE_BOTH_N)    \
+    X(KID_NORM_V8) X(KID_NORM_V16) X(KID_NORM_S16) X(KID_NORM_M) X(KID_NORM_W16)    \
+    X(KID_NORM_DX_V8) X(KID_NORM_DX_V16) X(KID_NORM_DX_S16) X(KID_NORM_DX_M) X(KID_NORM_DX_W16)    \
+    X(KID_NORM_DG_V8) X(KID_NORM_DG_V16) X(KID_NORM_DG_S16) X(KID_NORM_DG_M) X(KID_NORM_DG_W16)    \
+    X(KID_NORM_BOTH_V8) X(KID_NORM_BOTH_V16) X(KID_NORM_BOTH_S16) X(KID_NORM_BOTH_M) X(KID_NORM_BOTH_W16)    \
+    X(KID_DROPOUT) X(KID_POSITION_BIAS) X(KID_POSITION_BIAS_WGRAD)
 
 // A batch-norm epilogue is written into a task's argument block by type (C3Args or PwArgs, whose `ep` fields sit at
 // different offsets): the predicates that name the type must agree with the type the kernel takes.

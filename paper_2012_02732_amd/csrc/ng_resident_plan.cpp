@@ -118,6 +118,14 @@ double tile_round_us(const ng_graph* g, int v, int kid_any, int subs) {
             break;
         }
         case KID_ROPE_N: case KID_ROPE_DX_N: case KID_ROPE_DG_N: base = 2.0, per_tile = 0.3; break;
+        case KID_NORM_V8: case KID_NORM_V16: case KID_NORM_S16: {
+            const NormArgs* a = reinterpret_cast<const NormArgs*>(g->tasks[v].args);
+            base = 3.0, per_tile = 0.0003 * a->C * (1 << a->lanes_log2) * a->per_tile;    // quads of tokens through the memory pipeline
+            break;
+        }
+        case KID_DROPOUT: base = 1.5, per_tile = 0.4; break;
+        case KID_POSITION_BIAS: base = 1.2, per_tile = 0.1; break;
+        case KID_POSITION_BIAS_WGRAD: base = 1.5, per_tile = 0.3; break;
         case KID_ATTN_ROWS: base = 3.0, per_tile = 0.3; break;
         case KID_ATTN_W64: case KID_ATTN_W128: case KID_ATTN_DQ_W64: case KID_ATTN_DQ_W128: case KID_ATTN_DK_W64: case KID_ATTN_DK_W128:
         case KID_ATTN_DV_W64: case KID_ATTN_DV_W128: {

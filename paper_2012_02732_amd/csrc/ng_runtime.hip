@@ -88,7 +88,7 @@ int issue_all(ng_graph* g, bool multi) {
     if (!multi) {
         for (const SingleLaunch& l : g->single_launches) {
             void* args[1] = {const_cast<unsigned char*>(l.args.data())};
-            NG_HIP(hipLaunchKernel(l.fn, dim3(l.grid), dim3(kBlock), args, l.lds_bytes, origin));
+            NG_HIP(hipLaunchKernel(l.fn, dim3(l.grid), dim3(l.block), args, l.lds_bytes, origin));
         }
         return NG_OK;
     }
@@ -1218,7 +1218,7 @@ static bool executed_launch(const ng_graph* g, int id, int mode, SoloLaunch& out
         const SingleLaunch& l = g->single_launches[g->single_launch_of[id]];
         out = SoloLaunch();
         out.fn = l.fn, out.timed_fn = l.timed_fn, out.name = g->single_tasks[id].name;
-        out.grid = dim3(l.grid), out.lds_bytes = l.lds_bytes, out.args = l.args;
+        out.grid = dim3(l.grid), out.block = dim3(l.block), out.lds_bytes = l.lds_bytes, out.args = l.args;
         return true;
     }
     if (mode != NG_MODE_DEVICE_RESIDENT) {

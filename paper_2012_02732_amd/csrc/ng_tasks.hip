@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kBlock) void pack_pw_weights_k4_kernel(const float*
 }
 // Stand-alone kernel of one tile function: one workgroup per tile.
 template <int KID>
-__global__ __launch_bounds__(kBlock, min_waves(KID)) void standalone_kernel(typename KernelOf<KID>::Args a) {
+__global__ __launch_bounds__(block_threads(KID), min_waves(KID)) void standalone_kernel(typename KernelOf<KID>::Args a) {
     __shared__ __align__(16) float smem[smem_floats(KID)];
     NoWait wait;
     KernelOf<KID>::template tile<false>(a, blockIdx.x, smem, threadIdx.x, true, wait);
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kBlock, min_waves(KID)) void standalone_kernel(type
 // latest end minus the earliest start is the time the GPU is busy with the task when it runs alone,
 // without what the command processor spends around a dispatch.
 template <int KID>
-__global__ __launch_bounds__(kBlock, min_waves(KID)) void timed_kernel(typename KernelOf<KID>::Args a, unsigned long long* stamps) {
+__global__ __launch_bounds__(block_threads(KID), min_waves(KID)) void timed_kernel(typename KernelOf<KID>::Args a, unsigned long long* stamps) {
     __shared__ __align__(16) float smem[smem_floats(KID)];
     unsigned long long t0 = 0;
     if (threadIdx.x == 0) t0 = wall_clock64();
@@ -112,6 +112,7 @@ void set_kernel(Task& t, const typename KernelOf<KID>::Args& a, long ntiles) {
     t.args_bytes = sizeof(A);
     t.ntiles = ntiles;
     t.grid[0] = (unsigned)ntiles;
+    t.block[0] = block_threads(KID);
 }
 
 long ceil_div(long a, long b) { return (a + b - 1) / b; }
@@ -230,6 +231,11 @@ static int pair_kid(const Task& first, const Task& second) {
     if (kid_first == KID_ROPE_DX_4 && kid_second == KID_ROPE_DG_4) return KID_ROPE_BOTH_4;
     if (kid_first == KID_ROPE_DX_8 && kid_second == KID_ROPE_DG_8) return KID_ROPE_BOTH_8;
     if (kid_first == KID_ROPE_DX_N && kid_second == KID_ROPE_DG_N) return KID_ROPE_BOTH_N;
+    if (kid_first == KID_NORM_DX_V8 && kid_second == KID_NORM_DG_V8) return KID_NORM_BOTH_V8;
+    if (kid_first == KID_NORM_DX_V16 && kid_second == KID_NORM_DG_V16) return KID_NORM_BOTH_V16;
+    if (kid_first == KID_NORM_DX_S16 && kid_second == KID_NORM_DG_S16) return KID_NORM_BOTH_S16;
+    if (kid_first == KID_NORM_DX_M && kid_second == KID_NORM_DG_M) return KID_NORM_BOTH_M;
+    if (kid_first == KID_NORM_DX_W16 && kid_second == KID_NORM_DG_W16) return KID_NORM_BOTH_W16;
     return KID_NONE;
 }
 bool can_pair(const Task& first, const Task& second) {
@@ -274,10 +280,11 @@ static void set_pw_backward(const Task& dgrad, const Task& wgrad, Task& t) {
     t.block[0] = kBlock;
     set_kernel<KID>(t, p, pw_backward_tiles(p.na, p.nb, p.b.splits));
 }
-// Both gradients of norm and rotation: the walk of the weight gradient, whose workgroups leave rows of sums, with dx written on the way.
+// Both gradients of norm and rotation, or of a layer norm: the walk of the weight gradient, whose workgroups leave rows of sums, with dx
+// written on the way.
 template <int KID>
-static void set_rope_backward(const Task& dgrad, const Task& wgrad, Task& t) {
-    RopeArgs a, d;
+static void set_norm_backward(const Task& dgrad, const Task& wgrad, Task& t) {
+    typename KernelOf<KID>::Args a, d;
     std::memcpy(&a, wgrad.args, sizeof a);
     std::memcpy(&d, dgrad.args, sizeof d);
     a.y = d.y;
@@ -295,9 +302,14 @@ void make_pair_task(const Task& first, const Task& second, Task& t) {
             set_pair<KID_ATTN_DKV_T64>(first, second, t);
             t.ntiles = first.ntiles, t.grid[0] = (unsigned)first.ntiles;
             break;
-        case KID_ROPE_BOTH_4: set_rope_backward<KID_ROPE_BOTH_4>(first, second, t); break;
-        case KID_ROPE_BOTH_8: set_rope_backward<KID_ROPE_BOTH_8>(first, second, t); break;
-        case KID_ROPE_BOTH_N: set_rope_backward<KID_ROPE_BOTH_N>(first, second, t); break;
+        case KID_ROPE_BOTH_4: set_norm_backward<KID_ROPE_BOTH_4>(first, second, t); break;
+        case KID_ROPE_BOTH_8: set_norm_backward<KID_ROPE_BOTH_8>(first, second, t); break;
+        case KID_ROPE_BOTH_N: set_norm_backward<KID_ROPE_BOTH_N>(first, second, t); break;
+        case KID_NORM_BOTH_V8: set_norm_backward<KID_NORM_BOTH_V8>(first, second, t); break;
+        case KID_NORM_BOTH_V16: set_norm_backward<KID_NORM_BOTH_V16>(first, second, t); break;
+        case KID_NORM_BOTH_S16: set_norm_backward<KID_NORM_BOTH_S16>(first, second, t); break;
+        case KID_NORM_BOTH_M: set_norm_backward<KID_NORM_BOTH_M>(first, second, t); break;
+        case KID_NORM_BOTH_W16: set_norm_backward<KID_NORM_BOTH_W16>(first, second, t); break;
         default: t = first; break;
     }
 }
@@ -761,10 +773,75 @@ RopePlan rope_plan(const ng_graph* g, int v) {
     }
     return p;
 }
+// How a layer norm is computed: threads side by side along the tokens (wider accesses in a row, fewer channels in registers), and how
+// many blocks of tokens a workgroup walks.
+struct NormPlan {
+    int kid = KID_NONE;
+    int lanes_log2 = 0, blocks = 1, items = 1, per_tile = 1;
+    long tiles = 0;
+    size_t ws_floats = 0, cnt_words = 0;
+};
+bool is_norm_op(int op) { return op >= NG_OP_LAYER_NORM && op <= NG_OP_LAYER_NORM_WGRAD; }
+NormPlan norm_plan(const ng_graph* g, int v) {
+    NormPlan p;
+    const Node& nd = g->nodes[v];
+    if (!is_norm_op(nd.op)) return p;
+    const int which = nd.op - NG_OP_LAYER_NORM;                // forward, dgrad, wgrad
+    const Shape& x = g->nodes[nd.preds[which ? 1 : 0]].out;
+    const long C = x.c, T = x.h * x.w;
+    const bool wgrad = nd.op == NG_OP_LAYER_NORM_WGRAD;
+    auto one_of = [which](int forward, int dgrad, int wgrad) { return which == 0 ? forward : which == 1 ? dgrad : wgrad; };
+    const long quads = T >= 4 ? 4 : 1;
+    if (C > 4096 || (T < 4 && C * T > 4096)) {
+        p.kid = one_of(KID_NORM_M, KID_NORM_DX_M, KID_NORM_DG_M);
+        while (p.lanes_log2 < 4 && (1L << p.lanes_log2) < T) ++p.lanes_log2;
+        p.blocks = (int)ceil_div(T, 1L << p.lanes_log2);
+    } else if (T < 4) {
+        p.kid = one_of(KID_NORM_S16, KID_NORM_DX_S16, KID_NORM_DG_S16);
+        p.lanes_log2 = T == 1 ? 0 : T == 2 ? 1 : 2;
+    } else if (C > 1024 && x.n * ceil_div(T, 16) >= 256) {
+        p.kid = one_of(KID_NORM_W16, KID_NORM_DX_W16, KID_NORM_DG_W16);
+        p.lanes_log2 = 2;
+        p.blocks = (int)ceil_div(T, 16);
+    } else {
+        while (p.lanes_log2 < 3 && C * (2L << p.lanes_log2) <= 4096 && (quads << p.lanes_log2) < T) ++p.lanes_log2;
+        p.kid = C * (1L << p.lanes_log2) <= 8 * kBlock ? one_of(KID_NORM_V8, KID_NORM_DX_V8, KID_NORM_DG_V8) : one_of(KID_NORM_V16, KID_NORM_DX_V16, KID_NORM_DG_V16);
+        p.blocks = (int)ceil_div(T, quads << p.lanes_log2);
+    }
+    p.items = (int)(x.n * p.blocks);
+    p.per_tile = (int)ceil_div(p.items, wgrad ? 512 : 1L << 20);       // every workgroup of wgrad's leaves a row of sums that somebody has to add up
+    p.tiles = ceil_div(p.items, p.per_tile);
+    if (wgrad) {
+        p.ws_floats = (size_t)round64((p.tiles + row_groups((int)p.tiles)) * ((2 * C + 3) & ~3L));
+        p.cnt_words = (size_t)round64(1 + row_groups((int)p.tiles));
+    }
+    return p;
+}
+// Bucket of each distance -max_distance .. max_distance, -1 for keys that are not seen.
+std::vector<int> position_buckets(const ng_op_params& p) {
+    const int m = p.max_distance, b = p.both ? p.buckets / 2 : p.buckets, exact = b / 2;
+    std::vector<int> of(2 * (size_t)m + 1);
+    for (int d = -m; d <= m; ++d) {
+        const int far = d < 0 ? -d : d;
+        int at = far;
+        if (far >= exact) {
+            const double steps = std::log((double)far / exact) / std::log((double)m / exact) * (b - exact);
+            at = std::min(b - 1, exact + (int)std::floor(steps + 1e-9));
+        }
+        of[(size_t)(d + m)] = d > 0 ? (p.both ? b + at : -1) : at;
+    }
+    return of;
+}
+bool is_position_bias_op(int op) { return op == NG_OP_POSITION_BIAS || op == NG_OP_POSITION_BIAS_WGRAD; }
 }  // namespace
 
 size_t packed_floats(const ng_graph* g, int v) {
     const Node& nd = g->nodes[v];
+    if (is_norm_op(nd.op)) {
+        const NormPlan p = norm_plan(g, v);
+        return p.ws_floats + p.cnt_words;
+    }
+    if (is_position_bias_op(nd.op)) return 2 * (size_t)nd.p.max_distance + 1;      // the buckets
     if (is_attention_op(nd.op)) {
         const AttentionPlan p = attention_plan(g, v);
         return p.ws_floats + p.cnt_words + p.stats_floats;
@@ -795,7 +872,7 @@ size_t packed_floats(const ng_graph* g, int v) {
 }
 
 bool has_arrival_counters(int op) {
-    return op == NG_OP_CONV1X1_WGRAD || op == NG_OP_CONV3X3_WGRAD || op == NG_OP_DWCONV_WGRAD || op == NG_OP_BN_ACT_WGRAD || is_attention_op(op) || is_rope_op(op);
+    return op == NG_OP_CONV1X1_WGRAD || op == NG_OP_CONV3X3_WGRAD || op == NG_OP_DWCONV_WGRAD || op == NG_OP_BN_ACT_WGRAD || is_attention_op(op) || is_rope_op(op) || is_norm_op(op);
 }
 
 namespace {
@@ -813,14 +890,24 @@ hipError_t clear_words(float* p, size_t words, void* stream) {
 int pack_constants(ng_graph* g, int v, float* packed, void* stream) {
     const Node& nd = g->nodes[v];
     long wm, wn, wk;
-    if (is_attention_op(nd.op) || is_rope_op(nd.op)) {         // the arrival counters start at zero
+    if (is_attention_op(nd.op) || is_rope_op(nd.op) || is_norm_op(nd.op)) {    // the arrival counters start at zero
         const AttentionPlan p = attention_plan(g, v);
         const RopePlan r = rope_plan(g, v);
-        if (p.cnt_words + r.cnt_words == 0) return NG_OK;
-        const hipError_t e = clear_words(packed + p.ws_floats + r.ws_floats, p.cnt_words + r.cnt_words, stream);
-        if (e != hipSuccess) return g->fail(NG_EHIP, "clearing arrival counters of an attention operator: %s", hipGetErrorString(e));
+        const NormPlan m = norm_plan(g, v);
+        const size_t words = p.cnt_words + r.cnt_words + m.cnt_words;
+        if (words == 0) return NG_OK;
+        const hipError_t e = clear_words(packed + p.ws_floats + r.ws_floats + m.ws_floats, words, stream);
+        if (e != hipSuccess) return g->fail(NG_EHIP, "clearing arrival counters of an attention operator or a norm: %s", hipGetErrorString(e));
         return NG_OK;
     }
+    if (is_position_bias_op(nd.op)) {
+        const std::vector<int> of = position_buckets(nd.p);
+        hipError_t e = hipMemcpyAsync(packed, of.data(), of.size() * sizeof(int), hipMemcpyHostToDevice, static_cast<hipStream_t>(stream));
+        if (e == hipSuccess) e = hipStreamSynchronize(static_cast<hipStream_t>(stream));      // (the host's copy ends here)
+        if (e != hipSuccess) return g->fail(NG_EHIP, "copying the buckets of a position bias: %s", hipGetErrorString(e));
+        return NG_OK;
+    }
+    if (nd.op == NG_OP_DROPOUT) return NG_OK;
     if (wgrad_dims(g, v, &wm, &wn, &wk)) {                     // the arrival counters start at zero
         const WgradPlan p = wgrad_plan(g, v);
         if (p.cnt_words == 0) return NG_OK;
@@ -902,7 +989,7 @@ int build_task(ng_graph* g, int v, char* arena, float* packed, Task& t) {
 
     auto buf = [&](int id) { return reinterpret_cast<float*>(arena + g->offset[id]); };
     const Shape& o = nd.out;
-    const Shape& i0 = g->nodes[nd.preds[0]].out;
+    const Shape& i0 = nd.preds.empty() ? o : g->nodes[nd.preds[0]].out;
     const int total = (int)o.elems();
     const int hw_out = (int)(o.h * o.w);
     auto wf = [&](int j) { return static_cast<const float*>(nd.weights[j]); };
@@ -1365,6 +1452,49 @@ int build_task(ng_graph* g, int v, char* arena, float* packed, Task& t) {
             a.N = (int)q.n, a.H = nd.p.heads, a.Hk = nd.p.kv_heads, a.d = (int)(q.c / nd.p.heads), a.Tq = (int)(q.h * q.w), a.Tk = (int)(k.h * k.w);
             a.col_blocks = p.col_blocks, a.splits = p.splits, a.per_split = p.per_split;
             set_any_kernel(t, p.kid, a, p.tiles);
+            break;
+        }
+        case NG_OP_LAYER_NORM:
+        case NG_OP_LAYER_NORM_DGRAD:
+        case NG_OP_LAYER_NORM_WGRAD: {
+            const NormPlan p = norm_plan(g, v);
+            const bool backward = nd.op != NG_OP_LAYER_NORM;
+            const int first = backward ? 1 : 0;
+            const Shape& x = g->nodes[nd.preds[first]].out;
+            NormArgs a{};
+            a.x = buf(nd.preds[first]);
+            a.dy = backward ? buf(nd.preds[0]) : a.x;
+            a.gamma = wf(0), a.beta = wf(1);
+            a.y = buf(v), a.dg = buf(v);
+            if (p.cnt_words > 0) {
+                if (!packed) return g->fail(NG_EINVAL, "node %d: no workspace", v);
+                a.ws = packed, a.cnt = reinterpret_cast<unsigned*>(packed + p.ws_floats);
+            }
+            a.eps = nd.p.eps, a.C = (int)x.c, a.T = (int)(x.h * x.w);
+            a.lanes_log2 = p.lanes_log2, a.blocks = p.blocks, a.items = p.items, a.per_tile = p.per_tile, a.tiles = (int)p.tiles;
+            set_any_kernel(t, p.kid, a, p.tiles);
+            break;
+        }
+        case NG_OP_DROPOUT: {
+            DropoutArgs a{};
+            a.x = buf(nd.preds[0]), a.seed = buf(nd.preds[1]), a.y = buf(v);
+            if (nd.preds.size() > 2) a.residual = buf(nd.preds[2]);
+            const double limit = std::nearbyint((double)nd.p.rate * 4294967296.0);
+            a.total = o.elems(), a.site = (unsigned)nd.p.site, a.limit = (unsigned)limit, a.scale = (float)(4294967296.0 / (4294967296.0 - limit));
+            set_kernel<KID_DROPOUT>(t, a, ceil_div(a.total, kDropoutTile));
+            break;
+        }
+        case NG_OP_POSITION_BIAS:
+        case NG_OP_POSITION_BIAS_WGRAD: {
+            const bool wgrad = nd.op == NG_OP_POSITION_BIAS_WGRAD;
+            if (!packed) return g->fail(NG_EINVAL, "node %d: no buffer for the buckets", v);
+            PositionBiasArgs a{};
+            if (wgrad) a.dbias = buf(nd.preds[0]);
+            else a.table = wf(0);
+            a.bucket_of = reinterpret_cast<const int*>(packed), a.out = buf(v);
+            a.heads = nd.p.heads, a.distances = 2 * nd.p.max_distance + 1, a.buckets = nd.p.buckets;
+            if (wgrad) set_kernel<KID_POSITION_BIAS_WGRAD>(t, a, ceil_div((long)a.buckets * a.heads, kBlock / 64));
+            else set_kernel<KID_POSITION_BIAS>(t, a, ceil_div((long)a.heads * a.distances, kBlock));
             break;
         }
         default:

@@ -33,9 +33,15 @@ Conventions shared by every consumer (an interface, not an implementation):
                                             rotated in pairs by position * frequency
     attention       heads, kv_heads, scale; preds q, k, v and, if wanted, lengths [n, 1, 1, 1]: softmax
                                             attention of q's h x w tokens to those of k and v, heads as runs
-                                            of channels, keys j < lengths[image] only
+                                            of channels, keys j < lengths[image] only. With bias ('first'|'last')
+                                            the last pred is a bias [1, heads, 1, 2 m + 1] of the distance
+                                            j - i - offset (beyond m: as m), offset 0 or keys that count - queries
+    layer_norm      eps                     weights: gamma, beta [c]; over the channels of each pixel
+    dropout         rate, site              preds x, seed [1, 1, 1, 2] and, if wanted, a residual that is added
+    position_bias   heads, buckets, max_distance, both (0|1); no preds; weights: table [buckets, heads]
+                                            -> [1, heads, 1, 2 max_distance + 1]
 """
-from .model import Builder, Node, Workload, OPS, ATTENTION_OPS, TRAIN_OPS, rope_frequencies  # noqa: F401
+from .model import Builder, Node, Workload, OPS, ATTENTION_OPS, BLOCK_OPS, TRAIN_OPS, rope_frequencies  # noqa: F401
 from .configs import make, CONFIG_NAMES  # noqa: F401
 from .training import training_graph, nas_cell_cifar, TrainingWorkload  # noqa: F401
-from .attention import decoder_block  # noqa: F401
+from .attention import decoder_block, transformer_block  # noqa: F401

@@ -9,11 +9,13 @@ import numpy as np
 OPS = ("input", "conv1x1", "dwconv", "conv3x3", "bn_act", "relu", "add_n",
        "concat", "pool", "global_avgpool", "fc")
 ATTENTION_OPS = ("head_rope", "attention")
+BLOCK_OPS = ("layer_norm", "dropout", "position_bias")
 # operators that only occur in the DAG of a training iteration (see workloads/training.py)
 TRAIN_OPS = ("conv1x1_dgrad", "conv1x1_wgrad", "conv3x3_dgrad", "conv3x3_wgrad", "dwconv_dgrad", "dwconv_wgrad",
              "bn_act_dgrad", "bn_act_wgrad", "relu_dgrad", "pool_dgrad", "global_avgpool_dgrad", "channel_sum",
              "slice_pad", "sgd_update", "head_rope_dgrad", "head_rope_wgrad",
-             "attention_rows", "attention_dq", "attention_dk", "attention_dv")
+             "attention_rows", "attention_dq", "attention_dk", "attention_dv", "attention_dbias",
+             "layer_norm_dgrad", "layer_norm_wgrad", "position_bias_wgrad")
 
 
 @dataclass
@@ -149,14 +151,32 @@ class Builder:
         self.nodes[v].weights = [freq] + ([np.ones(c // heads, np.float32)] if norm else [])
         return v
 
-    def attention(self, q, k, v, heads, kv_heads=None, lengths=None, scale=None) -> int:
-        """Attention of q's tokens to the tokens of k and v; lengths [n, 1, 1, 1]: keys that count for each image."""
+    def attention(self, q, k, v, heads, kv_heads=None, lengths=None, scale=None, bias=None, at="first") -> int:
+        """Attention of q's tokens to the tokens of k and v; lengths [n, 1, 1, 1]: keys that count for each image; bias
+        [1, heads, 1, 2 m + 1]: added to the scores by the distance of key and query (``position_bias``), the first query at the first
+        key (``at`` "first") or the last one at the last key that counts ("last")."""
         n, c, h, w = self.shape(q)
         kv_heads = heads if kv_heads is None else kv_heads
         assert c % heads == 0 and self.shape(k) == self.shape(v) and self.shape(k)[:2] == (n, c // heads * kv_heads)
-        preds = [q, k, v] + ([] if lengths is None else [lengths])
+        preds = [q, k, v] + ([] if lengths is None else [lengths]) + ([] if bias is None else [bias])
+        how = {} if bias is None else {"bias": {"first": "first", "last": "last"}[at]}
         return self._add("attention", preds, (n, c, h, w), heads=heads, kv_heads=kv_heads,
-                         scale=float((c // heads) ** -0.5 if scale is None else scale))
+                         scale=float((c // heads) ** -0.5 if scale is None else scale), **how)
+
+    def layer_norm(self, x, eps=1e-5) -> int:
+        """Norm over the channels of each token (pixel)."""
+        return self._add("layer_norm", [x], self.shape(x), eps=float(eps))
+
+    def dropout(self, x, seed, rate, site, residual=None) -> int:
+        """Dropout of x (seed: an input [1, 1, 1, 2], site: which dropout of the network), added to ``residual`` if there is one."""
+        assert self.shape(seed) == (1, 1, 1, 2) and (residual is None or self.shape(residual) == self.shape(x))
+        return self._add("dropout", [x, seed] + ([] if residual is None else [residual]), self.shape(x), rate=float(rate), site=int(site))
+
+    def position_bias(self, heads, buckets=32, max_distance=128, both=True) -> int:
+        """Learned bias of the distance between key and query, [1, heads, 1, 2 max_distance + 1] (not ``both``: keys behind the query are
+        not seen)."""
+        return self._add("position_bias", [], (1, heads, 1, 2 * max_distance + 1), heads=heads, buckets=buckets, max_distance=max_distance,
+                         both=int(bool(both)))
 
     # -- values --------------------------------------------------------
     def draw_weights(self, rng: np.random.Generator, conv_std, bn_mode: str):
@@ -187,6 +207,12 @@ class Builder:
             elif nd.op == "head_rope" and len(nd.weights) > 1:
                 if bn_mode != "identity":
                     nd.weights[1] = rng.uniform(0.8, 1.2, nd.weights[1].shape).astype(np.float32)
+            elif nd.op == "layer_norm":
+                c = nd.shape[1]
+                nd.weights = [np.ones(c, np.float32), np.zeros(c, np.float32)] if bn_mode == "identity" else \
+                    [rng.uniform(0.8, 1.2, c).astype(np.float32), (rng.standard_normal(c) * 0.1).astype(np.float32)]
+            elif nd.op == "position_bias":
+                nd.weights = [rng.standard_normal((nd.params["buckets"], nd.params["heads"])).astype(np.float32)]
             elif nd.op == "bn_act":
                 c = nd.shape[1]
                 if bn_mode == "identity":

@@ -21,7 +21,11 @@ forward operator's input; weights are shared with the forward node):
     channel_sum           preds [dy]                                      -> [1, c, 1, 1]  (fc bias gradient)
     head_rope_dgrad / _wgrad preds [dy, x, positions]  the forward's parameters  shared frequencies, gamma; wgrad -> [1, d, 1, 1]
     attention_rows        preds [dy, y]    heads                           -> [n, 3 heads, h, w]
-    attention_dq / _dk / _dv preds [dy, rows, q, k, v(, lengths)]  heads, kv_heads, scale
+    attention_dq / _dk / _dv preds [dy, rows, q, k, v(, lengths)(, bias)]  heads, kv_heads, scale(, bias)
+    attention_dbias       preds as these, with a bias                     -> shape of the bias
+    layer_norm_dgrad / _wgrad preds [dy, x]  eps                          shared gamma, beta; wgrad -> [2, c, 1, 1]
+    dropout               preds [dy, seed]   rate, site of the forward operator
+    position_bias_wgrad   preds [dbias]      the forward's parameters     -> [buckets, heads, 1, 1]
     slice_pad             preds [dy]       cout, src_lo, src_hi, dst_lo   (gradient of one concat input)
     sgd_update            preds [grad, the other readers of the weight: its backward operator, its forward node]
                           lr, offset, numel                                shared W (written in place)
@@ -83,6 +87,10 @@ def training_graph(fwd: Workload, lr: float, seeds: Dict[int, np.ndarray]) -> Tr
         dy = c[0] if len(c) == 1 else add("add_n", c, nd.shape)
         grad_of[v] = dy
         p = nd.params
+        if nd.op == "position_bias":                        # reads its table only
+            wg = add("position_bias_wgrad", [dy], (p["buckets"], p["heads"], 1, 1), **{k: p[k] for k in ("heads", "buckets", "max_distance", "both")})
+            update(v, 0, wg, 0, p["buckets"] * p["heads"], [])
+            continue
         x = nd.preds[0]
         xs = fwd.nodes[x].shape
         want_dx = needs_grad[x]
@@ -125,13 +133,29 @@ def training_graph(fwd: Workload, lr: float, seeds: Dict[int, np.ndarray]) -> Tr
             if want_dx:
                 contrib[x].append(dx)
         elif nd.op == "attention":
-            if not any(needs_grad[u] for u in nd.preds[:3]):
+            biased = "bias" in p and needs_grad[nd.preds[-1]]
+            if not biased and not any(needs_grad[u] for u in nd.preds[:3]):
                 continue
-            how = {k: p[k] for k in ("heads", "kv_heads", "scale")}
+            how = {k: p[k] for k in ("heads", "kv_heads", "scale", "bias") if k in p}
             rows = add("attention_rows", [dy, v], (nd.shape[0], 3 * p["heads"]) + tuple(nd.shape[2:]), heads=p["heads"])
             for u, op in zip(nd.preds, ("attention_dq", "attention_dk", "attention_dv")):
                 if needs_grad[u]:
                     contrib[u].append(add(op, [dy, rows] + nd.preds, fwd.nodes[u].shape, **how))
+            if biased:
+                contrib[nd.preds[-1]].append(add("attention_dbias", [dy, rows] + nd.preds, fwd.nodes[nd.preds[-1]].shape, **how))
+        elif nd.op == "layer_norm":
+            shared = [(v, 0), (v, 1)]
+            dx = add("layer_norm_dgrad", [dy, x], xs, shared=shared, eps=p["eps"]) if want_dx else None
+            wg = add("layer_norm_wgrad", [dy, x], (2, xs[1], 1, 1), shared=shared, eps=p["eps"])
+            update(v, 0, wg, 0, xs[1], [dx])                # gamma
+            update(v, 1, wg, xs[1], xs[1], [dx])            # beta
+            if want_dx:
+                contrib[x].append(dx)
+        elif nd.op == "dropout":
+            if want_dx:
+                contrib[x].append(add("dropout", [dy, nd.preds[1]], xs, rate=p["rate"], site=p["site"]))
+            if len(nd.preds) > 2 and needs_grad[nd.preds[2]]:
+                contrib[nd.preds[2]].append(dy)
         elif nd.op == "relu":
             if want_dx:
                 contrib[x].append(add("relu_dgrad", [dy, x], xs))
