@@ -138,8 +138,17 @@ enum {
                                  the query are not seen: -infinity. e = b / 2 >= 1, e < m <= 1023:
                                    bucket(d) = |d| for |d| < e, else min(b - 1, e + floor((b - e) log(|d| / e) / log(m / e)))
                                  (in 64 bits; a border counts as reached from 1e-9 below it on) */
-    NG_OP_POSITION_BIAS_WGRAD = 38 /* preds {gradient of the bias, [1][heads][1][2 m + 1]}, no weights, same parameters -> dtable as
+    NG_OP_POSITION_BIAS_WGRAD = 38, /* preds {gradient of the bias, [1][heads][1][2 m + 1]}, no weights, same parameters -> dtable as
                                  [buckets][heads][1][1] */
+    /* With the parameter bias = 1 or 2, NG_OP_ATTENTION, _DQ, _DK and _DV take one pred more, the last: a bias [1][heads][1][2 m + 1], m <=
+     * 1023, from any node (NG_OP_POSITION_BIAS, or an input). The score of query i and key j of an image is scale <q[i], k[j]> +
+     * bias[head][distance], distance = j - i - offset held within -m .. m; offset 0 (bias = 1: the first query is where the keys begin) or
+     * keys that count less Tq (bias = 2: the last query is at the last key that counts, as when new tokens follow those of a cache).
+     * -infinity: the key is not seen by that query, and blocks of keys that no query sees cost nothing; a query that sees no key: 0.
+     * Other values are finite, up to 2^126 (NaN and +infinity spoil the queries that see them; the lowest values mask like large ones:
+     * a query with no other value gets the mean of these). */
+    NG_OP_ATTENTION_DBIAS = 39 /* preds {dy, rows, q, k, v[, lengths], bias} as for _DQ -> gradient of the bias, [1][heads][1][2 m + 1]: the sum
+                                 over images, queries and keys at each distance */
 };
 
 typedef struct ng_op_params {
@@ -163,6 +172,7 @@ typedef struct ng_op_params {
     int32_t site;      /* DROPOUT: >= 0; nodes with different sites have different masks under one seed */
     int32_t buckets;   /* POSITION_BIAS*: rows of the table */
     int32_t max_distance; /* POSITION_BIAS*: from here on distances have the last bucket; at most 1023 */
+    int32_t bias;      /* ATTENTION, _DQ, _DK, _DV, _DBIAS: 0 none, 1 distances from the first query at the first key, 2 from the last at the last */
     int32_t both;      /* POSITION_BIAS*: keys behind the query have buckets of their own (0: they are not seen) */
 } ng_op_params;
 
@@ -265,7 +275,7 @@ int ng_set_memory_reuse(ng_graph* g, int on);
  * and x) are computed in one walk over dy and x by the launch of whichever of the two comes first, if
  * both are on one stream (always, in modes 1 and 2); likewise the input gradient and the weight gradient
  * of a depthwise or 1 x 1 convolution (same dy) share one launch, their workgroups interleaved, if
- * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, those of NG_OP_LAYER_NORM, and dk and
+ * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, those of NG_OP_LAYER_NORM, dq and the bias's gradient of an attention with many queries, and dk and
  * dv of an attention with many keys and heads of up to 64 channels, with what both need computed once. In modes 1 and 2 tasks of the
  * same kernel that do not wait for each other share a launch as well, and the launches follow each other in an
  * order that lets them (ng_get_single_launches; attention operators' kernels have a launch each). on = 0 switches the exceptions off: one kernel per task. Call before ng_bind (NG_ESTATE after). */
@@ -364,7 +374,7 @@ enum {
                                    inputs were produced in place runs nothing (ng_resident_fusion reports which);
                                    every node's tensor is written all the same and equals the other modes' bit
                                    for bit. The plan passes a self-check at ng_capture or the capture fails.
-                                   A graph with attention operators has a plan if its tasks are small ones: no
+                                   A graph with attention operators (or norm, dropout and position bias) has a plan if its tasks are small ones: no
                                    attention over many queries (more than 768 pairs of 16 columns and 64 keys, where
                                    32 columns are exceeded), no kernel for large images, no gradients of convolutions
                                    and batch-norms. Without a plan the mode is no candidate of NG_MODE_AUTO, and this mode,

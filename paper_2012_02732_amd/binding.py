@@ -19,7 +19,8 @@ NG_OK, NG_EINVAL, NG_ESHAPE, NG_ESTATE, NG_ENOMEM, NG_EHIP = 0, -1, -2, -3, -4, 
  NG_OP_BN_ACT_DGRAD, NG_OP_BN_ACT_WGRAD, NG_OP_RELU_DGRAD, NG_OP_POOL_DGRAD, NG_OP_GAP_DGRAD, NG_OP_CHANNEL_SUM,
  NG_OP_SLICE_PAD, NG_OP_SGD_UPDATE, NG_OP_HEAD_ROPE, NG_OP_HEAD_ROPE_DGRAD, NG_OP_HEAD_ROPE_WGRAD,
  NG_OP_ATTENTION, NG_OP_ATTENTION_ROWS, NG_OP_ATTENTION_DQ, NG_OP_ATTENTION_DK, NG_OP_ATTENTION_DV,
- NG_OP_LAYER_NORM, NG_OP_LAYER_NORM_DGRAD, NG_OP_LAYER_NORM_WGRAD, NG_OP_DROPOUT, NG_OP_POSITION_BIAS, NG_OP_POSITION_BIAS_WGRAD) = range(39)
+ NG_OP_LAYER_NORM, NG_OP_LAYER_NORM_DGRAD, NG_OP_LAYER_NORM_WGRAD, NG_OP_DROPOUT, NG_OP_POSITION_BIAS, NG_OP_POSITION_BIAS_WGRAD,
+ NG_OP_ATTENTION_DBIAS) = range(40)
 NG_MODE_GRAPH_MULTI, NG_MODE_GRAPH_SINGLE, NG_MODE_EAGER_SINGLE, NG_MODE_EAGER_MULTI, NG_MODE_DEVICE_RESIDENT, NG_MODE_AUTO = range(6)
 NG_ASSIGN_ALGORITHM1, NG_ASSIGN_EXACT = 0, 1
 
@@ -42,7 +43,7 @@ class ng_op_params(C.Structure):
                 ("slice_lo", C.c_int32 * NG_MAX_PREDS), ("slice_hi", C.c_int32 * NG_MAX_PREDS), ("lr", C.c_float),
                 ("heads", C.c_int32), ("kv_heads", C.c_int32), ("rot", C.c_int32), ("interleaved", C.c_int32),
                 ("factor", C.c_float), ("scale", C.c_float), ("rate", C.c_float), ("site", C.c_int32), ("buckets", C.c_int32),
-                ("max_distance", C.c_int32), ("both", C.c_int32)]
+                ("max_distance", C.c_int32), ("bias", C.c_int32), ("both", C.c_int32)]
 
 
 if not os.path.exists(LIB_PATH):

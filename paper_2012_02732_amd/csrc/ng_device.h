@@ -68,9 +68,14 @@ enum Kid : int {
     KID_NORM_DX_V8, KID_NORM_DX_V16, KID_NORM_DX_S16, KID_NORM_DX_M, KID_NORM_DX_W16,
     KID_NORM_DG_V8, KID_NORM_DG_V16, KID_NORM_DG_S16, KID_NORM_DG_M, KID_NORM_DG_W16,
     KID_NORM_BOTH_V8, KID_NORM_BOTH_V16, KID_NORM_BOTH_S16, KID_NORM_BOTH_M, KID_NORM_BOTH_W16,
+    // attention with a bias of distances, launched kernels only: as above, and the bias's gradient (DB; DQB: with dq)
+    KID_ATTNB_W64, KID_ATTNB_W128, KID_ATTNB_DQ_W64, KID_ATTNB_DQ_W128, KID_ATTNB_DK_W64, KID_ATTNB_DK_W128, KID_ATTNB_DV_W64, KID_ATTNB_DV_W128,
+    KID_ATTNB_DB_W64, KID_ATTNB_DB_W128,
+    KID_ATTNB_T64, KID_ATTNB_T128, KID_ATTNB_DQ_T64, KID_ATTNB_DQ_T128, KID_ATTNB_DK_T64, KID_ATTNB_DK_T128, KID_ATTNB_DV_T64, KID_ATTNB_DV_T128,
+    KID_ATTNB_DB_T64, KID_ATTNB_DB_T128, KID_ATTNB_DQB_T64, KID_ATTNB_DQB_T128, KID_ATTNB_DKV_T64,
     KID_COUNT
 };
-constexpr bool is_attention_tile_kernel(int kid) { return kid >= KID_ATTN_T64 && kid <= KID_ATTN_DKV_T64; }
+constexpr bool is_attention_tile_kernel(int kid) { return (kid >= KID_ATTN_T64 && kid <= KID_ATTN_DKV_T64) || (kid >= KID_ATTNB_T64 && kid <= KID_ATTNB_DKV_T64); }
 constexpr bool is_launched_attention_kernel(int kid) { return kid >= KID_ATTN_T64 && kid < KID_COUNT; }
 constexpr bool is_attention_kernel(int kid) { return kid >= KID_ROPE_4 && kid < KID_COUNT; }
 constexpr bool is_wide_norm(int kid) { return kid == KID_NORM_W16 || kid == KID_NORM_DX_W16 || kid == KID_NORM_DG_W16 || kid == KID_NORM_BOTH_W16; }
@@ -99,7 +104,7 @@ constexpr bool is_c3_patch(int kid) { return kid >= KID_C3_P64 && kid <= KID_C3_
 constexpr int c3_patches(int kid) { return kid == KID_C3_SK ? 4 : kid == KID_C3_P64 || kid == KID_C3_P96 || kid == KID_C3_Q32 ? 2 : 1; }
 constexpr int c3_patch_pixels(int kid) { return kid == KID_C3_SK ? 160 : kid == KID_C3_Q64 ? 384 : kid == KID_C3_R32 || kid == KID_C3_R128 ? 640 : 256; }
 // wavefronts per SIMD that the registers of a stand-alone kernel must leave room for: the compiler takes more than half of them for 96 rows
-constexpr int min_waves(int kid) { return (is_c3_patch(kid) && kid != KID_C3_SK) || is_attention_tile_kernel(kid) || kid == KID_ATTN_W128 ? 2 : 1; }
+constexpr int min_waves(int kid) { return (is_c3_patch(kid) && kid != KID_C3_SK) || is_attention_tile_kernel(kid) || kid == KID_ATTN_W128 || kid == KID_ATTNB_W128 ? 2 : 1; }
 constexpr bool is_pw_columns(int kid) { return (kid >= KID_PW_V1 && kid <= KID_PW_S4) || kid == KID_PW_P32 || kid == KID_PW_P64; }   // tiles = row tiles x column blocks
 constexpr bool is_pw_patch(int kid) { return kid == KID_PW_P32 || kid == KID_PW_P64; }
 // windowed kernels for large tensors (batches): not in the lean build, but in the full and the train build
@@ -441,6 +446,13 @@ struct AttnArgs {
     int N, H, Hk, d, Tq, Tk;
     int col_blocks;            // blocks of columns (queries of the heads that share a key head; dk, dv: keys) for each image and key head
     int splits, per_split;     // the other side (keys; dk, dv: queries) is cut into splits of per_split blocks
+    // with a bias of distances
+    int reach, from_last;      // distances -reach .. reach; from_last: the last query is at the last key that counts
+    const float* bias;         // [H][2 reach + 1]
+    float* db;                 // its gradient
+    float* db_ws;              // for each head: sums of each workgroup [N query_blocks splits][2 reach + 1, rounded up to a multiple of four], then of groups
+    unsigned* db_cnt;          // for each head: arrivals, zero between replays
+    int query_blocks;          // blocks of columns (128, dbias by wavefronts: 16) of a head
 };
 
 // ---- around the attention of a block --------------------------------------------------------

@@ -243,10 +243,15 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
         case NG_OP_ATTENTION:
         case NG_OP_ATTENTION_DQ:
         case NG_OP_ATTENTION_DK:
-        case NG_OP_ATTENTION_DV: {
+        case NG_OP_ATTENTION_DV:
+        case NG_OP_ATTENTION_DBIAS: {
             const int first = op == NG_OP_ATTENTION ? 0 : 2;           // behind dy and rows
-            if ((n_preds != first + 3 && n_preds != first + 4) || n_weights != 0)
-                return first ? "attention backward takes dy, rows, q, k, v and, if the attention has them, lengths" : "attention takes q, k, v and, if wanted, lengths";
+            if (p.bias < 0 || p.bias > 2) return "attention: bias in {0, 1, 2}";
+            if (op == NG_OP_ATTENTION_DBIAS && p.bias == 0) return "attention_dbias: the attention has no bias";
+            const int biased = p.bias != 0, plain = n_preds - biased;  // the bias comes last
+            if ((plain != first + 3 && plain != first + 4) || n_weights != 0)
+                return first ? "attention backward takes dy, rows, q, k, v and, if the attention has them, lengths and a bias (with the parameter bias)"
+                             : "attention takes q, k, v and, if wanted, lengths and a bias (with the parameter bias)";
             const Shape &q = in(first), &k = in(first + 1), &v = in(first + 2);
             if (p.heads <= 0 || p.kv_heads <= 0 || p.heads % p.kv_heads != 0) return "attention: kv_heads must be positive and divide heads";
             if (!std::isfinite((float)(p.scale * 1.4426950408889634)) || p.scale == 0.f) return "attention: scale must be finite, also times log2 e, and not 0";
@@ -259,17 +264,21 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
             if (Tq * d * (p.heads / p.kv_heads) > kMaxSliceElems || Tk * d > kMaxSliceElems)
                 return "attention: a head of k, or the heads of q that read it, have more than 2^29 values";
             if (q.n * p.kv_heads * ((std::max(Tq * (p.heads / p.kv_heads), Tk) + 15) / 16) > kMaxAttentionTiles) return "attention: too many heads and tokens for one launch";
-            if (n_preds == first + 4 && !(in(first + 3) == Shape{q.n, 1, 1, 1})) return "attention: lengths must be [n][1][1][1]";
+            if (plain == first + 4 && !(in(first + 3) == Shape{q.n, 1, 1, 1})) return "attention: lengths must be [n][1][1][1]";
+            const Shape bias = biased ? in(n_preds - 1) : Shape{};
+            if (biased && (!(bias == Shape{1, p.heads, 1, bias.w}) || bias.w % 2 != 1 || bias.w > 2 * kMaxReach + 1))
+                return "attention: the bias must be [1][heads][1][2 m + 1], m at most 1023";
+            if (biased && q.n * p.heads * ((Tq + 15) / 16) > kMaxAttentionTiles) return "attention: too many heads and queries for one launch";
             if (first) {
                 if (!(in(0) == q)) return "attention backward: dy and q differ in shape";
                 const Node& rows = g->nodes[preds[1]];
                 code = NG_EINVAL;
                 if (rows.op != NG_OP_ATTENTION_ROWS || rows.preds[0] != preds[0]) return "attention backward: the second input must be the attention_rows node of dy";
                 const Node& y = g->nodes[rows.preds[1]];
-                if (y.preds != std::vector<int>(preds + 2, preds + n_preds) || y.p.heads != p.heads || y.p.kv_heads != p.kv_heads || y.p.scale != p.scale)
-                    return "attention backward: rows are of an attention with other inputs, heads or scale";
+                if (y.preds != std::vector<int>(preds + 2, preds + n_preds) || y.p.heads != p.heads || y.p.kv_heads != p.kv_heads || y.p.scale != p.scale || y.p.bias != p.bias)
+                    return "attention backward: rows are of an attention with other inputs, heads, scale or bias";
             }
-            out = op == NG_OP_ATTENTION_DK || op == NG_OP_ATTENTION_DV ? k : q;
+            out = op == NG_OP_ATTENTION_DBIAS ? bias : op == NG_OP_ATTENTION_DK || op == NG_OP_ATTENTION_DV ? k : q;
             return nullptr;
         }
         case NG_OP_ATTENTION_ROWS: {
@@ -663,12 +672,14 @@ int ng_task_work(const ng_graph* g, int id, double* bytes, double* flops) {
         case NG_OP_ATTENTION:
         case NG_OP_ATTENTION_DQ:
         case NG_OP_ATTENTION_DK:
-        case NG_OP_ATTENTION_DV: {                                  // products over every query and key: all there can be
+        case NG_OP_ATTENTION_DV:
+        case NG_OP_ATTENTION_DBIAS: {                               // products over every query and key: all there can be
             const int first = nd.op == NG_OP_ATTENTION ? 0 : 2;
             const Shape& k = g->nodes[nd.preds[first + 1]].out;
             const double q = (double)g->nodes[nd.preds[first]].out.elems();
             b = 4 * ((first ? 2 : 1) * q + 2 * (double)k.elems() + out);
-            f = 2 * q * (double)(k.h * k.w) * (nd.op == NG_OP_ATTENTION || nd.op == NG_OP_ATTENTION_DV ? 2 : 3);
+            if (nd.p.bias != 0) b += 4 * (double)g->nodes[nd.preds.back()].out.elems();
+            f = 2 * q * (double)(k.h * k.w) * (nd.op == NG_OP_ATTENTION_DQ || nd.op == NG_OP_ATTENTION_DK ? 3 : 2);
             break;
         }
         case NG_OP_ATTENTION_ROWS: b = 4 * (2 * in0 + out), f = 2 * in0; break;

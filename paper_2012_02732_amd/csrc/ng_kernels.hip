@@ -103,9 +103,9 @@ constexpr int kSmemFloats = 5120;
 // ... and what the patch-stationary kernels get instead: 24 floats (16 channels in three bf16 parts) for every pixel of their patches,
 // 640 at most. Stand-alone kernels: only they; the resident kernel: every workgroup of the build that contains them.
 constexpr int kSmemFloatsPatch = 24 * 256, kSmemFloatsWide = 24 * 640;
-constexpr int attention_tile_floats(int kid);                  // ng_attention_tiles.inc
+constexpr int attention_tile_floats(int kid), dbias_wave_floats();      // ng_attention_tiles.inc
 constexpr int smem_floats(int kid) {
-    return is_attention_tile_kernel(kid) ? attention_tile_floats(kid) : is_c3_patch(kid) ? 24 * c3_patches(kid) * c3_patch_pixels(kid) : kid == KID_PW_P32 ? 2 * kSmemFloatsPatch : is_pw_patch(kid) ? kSmemFloatsPatch : kSmemFloats;
+    return is_attention_tile_kernel(kid) ? attention_tile_floats(kid) : kid == KID_ATTNB_DB_W64 || kid == KID_ATTNB_DB_W128 ? dbias_wave_floats() : is_c3_patch(kid) ? 24 * c3_patches(kid) * c3_patch_pixels(kid) : kid == KID_PW_P32 ? 2 * kSmemFloatsPatch : is_pw_patch(kid) ? kSmemFloatsPatch : kSmemFloats;
 }
 
 // ------------------------------------------------------------------------------------
@@ -2011,23 +2011,23 @@ NG_KERNEL(KID_ROPE_DX_N, RopeArgs, "head_rope_dgrad_few", rope_few_tile < ROPE_D
 NG_KERNEL(KID_ROPE_DG_4, RopeArgs, "head_rope_wgrad_128", rope_tile < ROPE_DG, 4)
 NG_KERNEL(KID_ROPE_DG_8, RopeArgs, "head_rope_wgrad_256", rope_tile < ROPE_DG, 8)
 NG_KERNEL(KID_ROPE_DG_N, RopeArgs, "head_rope_wgrad_few", rope_few_tile < ROPE_DG)
-NG_KERNEL(KID_ATTN_W64, AttnArgs, "attention_wave_64", attention_wave_tile < 4)
-NG_KERNEL(KID_ATTN_W128, AttnArgs, "attention_wave_128", attention_wave_tile < 8)
-NG_KERNEL(KID_ATTN_DQ_W64, AttnArgs, "attention_dq_wave_64", attention_dq_wave_tile < 4)
-NG_KERNEL(KID_ATTN_DQ_W128, AttnArgs, "attention_dq_wave_128", attention_dq_wave_tile < 8)
-NG_KERNEL(KID_ATTN_DK_W64, AttnArgs, "attention_dk_wave_64", attention_dkv_wave_tile < 4, true)
-NG_KERNEL(KID_ATTN_DK_W128, AttnArgs, "attention_dk_wave_128", attention_dkv_wave_tile < 8, true)
-NG_KERNEL(KID_ATTN_DV_W64, AttnArgs, "attention_dv_wave_64", attention_dkv_wave_tile < 4, false)
-NG_KERNEL(KID_ATTN_DV_W128, AttnArgs, "attention_dv_wave_128", attention_dkv_wave_tile < 8, false)
-NG_KERNEL(KID_ATTN_T64, AttnArgs, "attention_tile_64", attention_tile < 64)
-NG_KERNEL(KID_ATTN_T128, AttnArgs, "attention_tile_128", attention_tile < 128)
-NG_KERNEL(KID_ATTN_DQ_T64, AttnArgs, "attention_dq_tile_64", attention_dq_tile < 64)
-NG_KERNEL(KID_ATTN_DQ_T128, AttnArgs, "attention_dq_tile_128", attention_dq_tile < 128)
-NG_KERNEL(KID_ATTN_DK_T64, AttnArgs, "attention_dk_tile_64", attention_dk_tile < 64)
-NG_KERNEL(KID_ATTN_DK_T128, AttnArgs, "attention_dk_tile_128", attention_dk_tile < 128)
-NG_KERNEL(KID_ATTN_DV_T64, AttnArgs, "attention_dv_tile_64", attention_dv_tile < 64)
-NG_KERNEL(KID_ATTN_DV_T128, AttnArgs, "attention_dv_tile_128", attention_dv_tile < 128)
-NG_KERNEL(KID_ATTN_DKV_T64, PairAttnArgs, "attention_dk+dv_tile_64", attention_dk_dv_tile < 64)
+NG_KERNEL(KID_ATTN_W64, AttnArgs, "attention_wave_64", attention_wave_tile < 4, false)
+NG_KERNEL(KID_ATTN_W128, AttnArgs, "attention_wave_128", attention_wave_tile < 8, false)
+NG_KERNEL(KID_ATTN_DQ_W64, AttnArgs, "attention_dq_wave_64", attention_dq_wave_tile < 4, false)
+NG_KERNEL(KID_ATTN_DQ_W128, AttnArgs, "attention_dq_wave_128", attention_dq_wave_tile < 8, false)
+NG_KERNEL(KID_ATTN_DK_W64, AttnArgs, "attention_dk_wave_64", attention_dkv_wave_tile < 4, true, false)
+NG_KERNEL(KID_ATTN_DK_W128, AttnArgs, "attention_dk_wave_128", attention_dkv_wave_tile < 8, true, false)
+NG_KERNEL(KID_ATTN_DV_W64, AttnArgs, "attention_dv_wave_64", attention_dkv_wave_tile < 4, false, false)
+NG_KERNEL(KID_ATTN_DV_W128, AttnArgs, "attention_dv_wave_128", attention_dkv_wave_tile < 8, false, false)
+NG_KERNEL(KID_ATTN_T64, AttnArgs, "attention_tile_64", attention_tile < 64, false)
+NG_KERNEL(KID_ATTN_T128, AttnArgs, "attention_tile_128", attention_tile < 128, false)
+NG_KERNEL(KID_ATTN_DQ_T64, AttnArgs, "attention_dq_tile_64", attention_dq_tile < 64, true, false, false)
+NG_KERNEL(KID_ATTN_DQ_T128, AttnArgs, "attention_dq_tile_128", attention_dq_tile < 128, true, false, false)
+NG_KERNEL(KID_ATTN_DK_T64, AttnArgs, "attention_dk_tile_64", attention_dk_tile < 64, false)
+NG_KERNEL(KID_ATTN_DK_T128, AttnArgs, "attention_dk_tile_128", attention_dk_tile < 128, false)
+NG_KERNEL(KID_ATTN_DV_T64, AttnArgs, "attention_dv_tile_64", attention_dv_tile < 64, false)
+NG_KERNEL(KID_ATTN_DV_T128, AttnArgs, "attention_dv_tile_128", attention_dv_tile < 128, false)
+NG_KERNEL(KID_ATTN_DKV_T64, PairAttnArgs, "attention_dk+dv_tile_64", attention_dk_dv_tile < 64, false)
 NG_KERNEL(KID_ROPE_BOTH_4, RopeArgs, "head_rope_dgrad+wgrad_128", rope_tile < ROPE_BOTH, 4)
 NG_KERNEL(KID_ROPE_BOTH_8, RopeArgs, "head_rope_dgrad+wgrad_256", rope_tile < ROPE_BOTH, 8)
 NG_KERNEL(KID_ROPE_BOTH_N, RopeArgs, "head_rope_dgrad+wgrad_few", rope_few_tile < ROPE_BOTH)
@@ -2051,6 +2051,29 @@ NG_KERNEL(KID_NORM_BOTH_V16, NormArgs, "layer_norm_dgrad+wgrad_16", norm_tile < 
 NG_KERNEL(KID_NORM_BOTH_S16, NormArgs, "layer_norm_dgrad+wgrad_few", norm_tile < NORM_BOTH, 256, 1, 16)
 NG_KERNEL(KID_NORM_BOTH_M, NormArgs, "layer_norm_dgrad+wgrad_many", norm_many_tile < NORM_BOTH)
 NG_KERNEL(KID_NORM_BOTH_W16, NormArgs, "layer_norm_dgrad+wgrad_wide", norm_tile < NORM_BOTH, 1024, 4, 16)
+NG_KERNEL(KID_ATTNB_W64, AttnArgs, "attention_biased_wave_64", attention_wave_tile < 4, true)
+NG_KERNEL(KID_ATTNB_W128, AttnArgs, "attention_biased_wave_128", attention_wave_tile < 8, true)
+NG_KERNEL(KID_ATTNB_DQ_W64, AttnArgs, "attention_biased_dq_wave_64", attention_dq_wave_tile < 4, true)
+NG_KERNEL(KID_ATTNB_DQ_W128, AttnArgs, "attention_biased_dq_wave_128", attention_dq_wave_tile < 8, true)
+NG_KERNEL(KID_ATTNB_DK_W64, AttnArgs, "attention_biased_dk_wave_64", attention_dkv_wave_tile < 4, true, true)
+NG_KERNEL(KID_ATTNB_DK_W128, AttnArgs, "attention_biased_dk_wave_128", attention_dkv_wave_tile < 8, true, true)
+NG_KERNEL(KID_ATTNB_DV_W64, AttnArgs, "attention_biased_dv_wave_64", attention_dkv_wave_tile < 4, false, true)
+NG_KERNEL(KID_ATTNB_DV_W128, AttnArgs, "attention_biased_dv_wave_128", attention_dkv_wave_tile < 8, false, true)
+NG_KERNEL(KID_ATTNB_T64, AttnArgs, "attention_biased_tile_64", attention_tile < 64, true)
+NG_KERNEL(KID_ATTNB_T128, AttnArgs, "attention_biased_tile_128", attention_tile < 128, true)
+NG_KERNEL(KID_ATTNB_DQ_T64, AttnArgs, "attention_biased_dq_tile_64", attention_dq_tile < 64, true, false, true)
+NG_KERNEL(KID_ATTNB_DQ_T128, AttnArgs, "attention_biased_dq_tile_128", attention_dq_tile < 128, true, false, true)
+NG_KERNEL(KID_ATTNB_DK_T64, AttnArgs, "attention_biased_dk_tile_64", attention_dk_tile < 64, true)
+NG_KERNEL(KID_ATTNB_DK_T128, AttnArgs, "attention_biased_dk_tile_128", attention_dk_tile < 128, true)
+NG_KERNEL(KID_ATTNB_DV_T64, AttnArgs, "attention_biased_dv_tile_64", attention_dv_tile < 64, true)
+NG_KERNEL(KID_ATTNB_DV_T128, AttnArgs, "attention_biased_dv_tile_128", attention_dv_tile < 128, true)
+NG_KERNEL(KID_ATTNB_DKV_T64, PairAttnArgs, "attention_biased_dk+dv_tile_64", attention_dk_dv_tile < 64, true)
+NG_KERNEL(KID_ATTNB_DB_W64, AttnArgs, "attention_dbias_wave_64", attention_dbias_wave_tile < 4)
+NG_KERNEL(KID_ATTNB_DB_T64, AttnArgs, "attention_dbias_tile_64", attention_dq_tile < 64, false, true, true)
+NG_KERNEL(KID_ATTNB_DQB_T64, AttnArgs, "attention_biased_dq+dbias_tile_64", attention_dq_tile < 64, true, true, true)
+NG_KERNEL(KID_ATTNB_DB_W128, AttnArgs, "attention_dbias_wave_128", attention_dbias_wave_tile < 8)
+NG_KERNEL(KID_ATTNB_DB_T128, AttnArgs, "attention_dbias_tile_128", attention_dq_tile < 128, false, true, true)
+NG_KERNEL(KID_ATTNB_DQB_T128, AttnArgs, "attention_biased_dq+dbias_tile_128", attention_dq_tile < 128, true, true, true)
 #undef NG_KERNEL
 NG_KERNEL0(KID_ATTN_ROWS, AttnArgs, "attention_rows", attention_rows_tile)
 NG_KERNEL0(KID_DROPOUT, DropoutArgs, "dropout", dropout_tile)
@@ -2085,7 +2108,11 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_NORM_DX_V8) X(KID_NORM_DX_V16) X(KID_NORM_DX_S16) X(KID_NORM_DX_M) X(KID_NORM_DX_W16)    \
     X(KID_NORM_DG_V8) X(KID_NORM_DG_V16) X(KID_NORM_DG_S16) X(KID_NORM_DG_M) X(KID_NORM_DG_W16)    \
     X(KID_NORM_BOTH_V8) X(KID_NORM_BOTH_V16) X(KID_NORM_BOTH_S16) X(KID_NORM_BOTH_M) X(KID_NORM_BOTH_W16)    \
-    X(KID_DROPOUT) X(KID_POSITION_BIAS) X(KID_POSITION_BIAS_WGRAD)
+    X(KID_DROPOUT) X(KID_POSITION_BIAS) X(KID_POSITION_BIAS_WGRAD)    \
+    X(KID_ATTNB_W64) X(KID_ATTNB_W128) X(KID_ATTNB_DQ_W64) X(KID_ATTNB_DQ_W128) X(KID_ATTNB_DK_W64) X(KID_ATTNB_DK_W128)    \
+    X(KID_ATTNB_DV_W64) X(KID_ATTNB_DV_W128) X(KID_ATTNB_T64) X(KID_ATTNB_T128) X(KID_ATTNB_DQ_T64) X(KID_ATTNB_DQ_T128)    \
+    X(KID_ATTNB_DK_T64) X(KID_ATTNB_DK_T128) X(KID_ATTNB_DV_T64) X(KID_ATTNB_DV_T128) X(KID_ATTNB_DKV_T64) X(KID_ATTNB_DB_W64)    \
+    X(KID_ATTNB_DB_T64) X(KID_ATTNB_DQB_T64) X(KID_ATTNB_DB_W128) X(KID_ATTNB_DB_T128) X(KID_ATTNB_DQB_T128)
 
 // A batch-norm epilogue is written into a task's argument block by type (C3Args or PwArgs, whose `ep` fields sit at
 // different offsets): the predicates that name the type must agree with the type the kernel takes.

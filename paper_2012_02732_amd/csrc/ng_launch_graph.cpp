@@ -19,7 +19,7 @@ namespace ng {
 // Two attention operators' parameters agree.
 static bool same_attention(const ng_op_params& a, const ng_op_params& b) {
     return a.heads == b.heads && a.kv_heads == b.kv_heads && a.rot == b.rot && a.interleaved == b.interleaved && a.eps == b.eps && a.factor == b.factor &&
-           a.scale == b.scale;
+           a.scale == b.scale && a.bias == b.bias;
 }
 
 // Which tasks have no launch of their own in modes 0-3:
@@ -31,8 +31,8 @@ static bool same_attention(const ng_op_params& a, const ng_op_params& b) {
 //     (`one_stream`: of the whole submission order; fused_into[v] = that update). A later launch is always in order
 //     for an update: it already comes after every reader of its weights, and it keeps its place in the stream, so
 //     the last one's launch comes after everything the earlier ones waited for;
-//   * the input gradient and gamma's gradient of a norm and rotation of heads, those of a layer norm, and dk and dv of an attention with heads of up to 64
-//     channels, likewise share a launch with the work that both need done once;
+//   * the input gradient and gamma's gradient of a norm and rotation of heads, those of a layer norm, dk and dv of an attention with heads of up to 64
+//     channels, and dq of an attention with many queries and its bias's gradient, likewise share a launch with the work that both need done once;
 //   * the input gradient and the parameter gradients of a batch-norm (same dy, same x) are computed by one launch, at
 //     the place of whichever of the two tasks comes first on their stream (fused_into[the later one] = the earlier
 //     one). Both are ready when the first one is (same inputs), each tensor has its buffer to itself, and the later
@@ -105,10 +105,10 @@ void decide_launch_fusion(const ng_graph* g, const std::vector<Task>& tasks, boo
             break;
         }
     }
-    // the gradients of a norm and rotation, those of a layer norm, and dk and dv of an attention, read the same tensors: one launch, at the
-    // place of whichever comes first (everything they read comes before both)
+    // the gradients of a norm and rotation, those of a layer norm, dk and dv of an attention, and its dq and its bias's gradient, read the
+    // same tensors: one launch, at the place of whichever comes first (everything they read comes before both)
     auto partner = [](int op) {
-        return op == NG_OP_HEAD_ROPE_DGRAD ? NG_OP_HEAD_ROPE_WGRAD : op == NG_OP_LAYER_NORM_DGRAD ? NG_OP_LAYER_NORM_WGRAD : op == NG_OP_ATTENTION_DK ? NG_OP_ATTENTION_DV : NG_OP_INPUT;
+        return op == NG_OP_HEAD_ROPE_DGRAD ? NG_OP_HEAD_ROPE_WGRAD : op == NG_OP_LAYER_NORM_DGRAD ? NG_OP_LAYER_NORM_WGRAD : op == NG_OP_ATTENTION_DK ? NG_OP_ATTENTION_DV : op == NG_OP_ATTENTION_DQ ? NG_OP_ATTENTION_DBIAS : NG_OP_INPUT;
     };
     for (int d = 0; d < n; ++d) {
         const Node& nd = g->nodes[d];

@@ -228,6 +228,9 @@ static int pair_kid(const Task& first, const Task& second) {
     if (kid_first == KID_PW_PX_DGRAD && kid_second == KID_PW_WGRAD_PX) return KID_PAIR_PW16;
     if (kid_first == KID_PW_PX_DGRAD && kid_second == KID_PW_WGRAD_PX2) return KID_PAIR_PW32;
     if (kid_first == KID_ATTN_DK_T64 && kid_second == KID_ATTN_DV_T64) return KID_ATTN_DKV_T64;
+    if (kid_first == KID_ATTNB_DK_T64 && kid_second == KID_ATTNB_DV_T64) return KID_ATTNB_DKV_T64;
+    if (kid_first == KID_ATTNB_DQ_T64 && kid_second == KID_ATTNB_DB_T64) return KID_ATTNB_DQB_T64;
+    if (kid_first == KID_ATTNB_DQ_T128 && kid_second == KID_ATTNB_DB_T128) return KID_ATTNB_DQB_T128;
     if (kid_first == KID_ROPE_DX_4 && kid_second == KID_ROPE_DG_4) return KID_ROPE_BOTH_4;
     if (kid_first == KID_ROPE_DX_8 && kid_second == KID_ROPE_DG_8) return KID_ROPE_BOTH_8;
     if (kid_first == KID_ROPE_DX_N && kid_second == KID_ROPE_DG_N) return KID_ROPE_BOTH_N;
@@ -240,7 +243,7 @@ static int pair_kid(const Task& first, const Task& second) {
 }
 bool can_pair(const Task& first, const Task& second) {
     const int kid = pair_kid(first, second);
-    if (kid != KID_ATTN_DKV_T64) return kid != KID_NONE;
+    if (!is_attention_tile_kernel(kid)) return kid != KID_NONE;
     AttnArgs a, b;                                             // its workgroups are cut in one way for both
     std::memcpy(&a, first.args, sizeof a);
     std::memcpy(&b, second.args, sizeof b);
@@ -292,6 +295,17 @@ static void set_norm_backward(const Task& dgrad, const Task& wgrad, Task& t) {
     t.block[0] = kBlock;
     set_kernel<KID>(t, a, wgrad.ntiles);
 }
+// dq's task with the result and the rows of sums of the bias's gradient.
+template <int KID>
+static void set_dq_dbias(const Task& dq, const Task& dbias, Task& t) {
+    AttnArgs a, b;
+    std::memcpy(&a, dq.args, sizeof a);
+    std::memcpy(&b, dbias.args, sizeof b);
+    a.db = b.db, a.db_ws = b.db_ws, a.db_cnt = b.db_cnt;
+    t = Task();
+    t.block[0] = kBlock;
+    set_kernel<KID>(t, a, dq.ntiles);
+}
 void make_pair_task(const Task& first, const Task& second, Task& t) {
     switch (pair_kid(first, second)) {
         case KID_PAIR_DW: set_pair<KID_PAIR_DW>(first, second, t); break;
@@ -302,6 +316,12 @@ void make_pair_task(const Task& first, const Task& second, Task& t) {
             set_pair<KID_ATTN_DKV_T64>(first, second, t);
             t.ntiles = first.ntiles, t.grid[0] = (unsigned)first.ntiles;
             break;
+        case KID_ATTNB_DKV_T64:
+            set_pair<KID_ATTNB_DKV_T64>(first, second, t);
+            t.ntiles = first.ntiles, t.grid[0] = (unsigned)first.ntiles;
+            break;
+        case KID_ATTNB_DQB_T64: set_dq_dbias<KID_ATTNB_DQB_T64>(first, second, t); break;
+        case KID_ATTNB_DQB_T128: set_dq_dbias<KID_ATTNB_DQB_T128>(first, second, t); break;
         case KID_ROPE_BOTH_4: set_norm_backward<KID_ROPE_BOTH_4>(first, second, t); break;
         case KID_ROPE_BOTH_8: set_norm_backward<KID_ROPE_BOTH_8>(first, second, t); break;
         case KID_ROPE_BOTH_N: set_norm_backward<KID_ROPE_BOTH_N>(first, second, t); break;
@@ -658,11 +678,11 @@ WgradPlan wgrad_plan(const ng_graph* g, int v) {
 long round64(long n) { return (n + 63) & ~63L; }
 struct AttentionPlan {
     int kid = KID_NONE;
-    int col_blocks = 1, splits = 1, per_split = 1;
+    int col_blocks = 1, splits = 1, per_split = 1, query_blocks = 1;
     long tiles = 0;
     size_t ws_floats = 0, cnt_words = 0, stats_floats = 0;
 };
-bool is_attention_op(int op) { return op >= NG_OP_ATTENTION && op <= NG_OP_ATTENTION_DV; }
+bool is_attention_op(int op) { return (op >= NG_OP_ATTENTION && op <= NG_OP_ATTENTION_DV) || op == NG_OP_ATTENTION_DBIAS; }
 // Splits of a tile kernel's other side: the number with which the task is expected to end first. A compute unit has two workgroups at a
 // time, which take longer than one alone, but not twice as long; a last one that is left over has it to itself. A split costs what the
 // workgroup that joins them reads. us, of the straight lines through what these kernels take with 1 .. 32 splits: 47 queries of 28 heads
@@ -670,7 +690,7 @@ bool is_attention_op(int op) { return op >= NG_OP_ATTENTION && op <= NG_OP_ATTEN
 // 93 keys of 13 heads of 96, 6892 queries each, 8 127, 16 80, 32 86.
 long tile_splits(int op, bool narrow, long groups, long blocks) {
     const bool by_keys = op == NG_OP_ATTENTION_DK || op == NG_OP_ATTENTION_DV, both = by_keys && narrow;      // both: one launch, cut alike
-    const bool heavy = !narrow && (op == NG_OP_ATTENTION_DQ || op == NG_OP_ATTENTION_DK);
+    const bool heavy = !narrow && (op == NG_OP_ATTENTION_DQ || op == NG_OP_ATTENTION_DBIAS || op == NG_OP_ATTENTION_DK);
     const double one = heavy ? 4.4 : both ? 3.4 : 2.0;             // a block of a workgroup that is alone
     const double pair = heavy ? 5.8 : both ? 4.4 : narrow ? 2.5 : 3.2;      // of two
     const double around = heavy ? 8.0 : 6.0;                       // first loads, results
@@ -695,8 +715,12 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     const long d = q.c / nd.p.heads, group = nd.p.heads / nd.p.kv_heads, Tq = q.h * q.w, Tk = k.h * k.w;
     const bool by_keys = nd.op == NG_OP_ATTENTION_DK || nd.op == NG_OP_ATTENTION_DV;
     const bool narrow = d <= 64;
-    p.kid = nd.op == NG_OP_ATTENTION ? (narrow ? KID_ATTN_W64 : KID_ATTN_W128) : nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_W64 : KID_ATTN_DQ_W128)
-          : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_W64 : KID_ATTN_DK_W128) : (narrow ? KID_ATTN_DV_W64 : KID_ATTN_DV_W128);
+    const bool biased = nd.p.bias != 0, dbias = nd.op == NG_OP_ATTENTION_DBIAS;
+    // the kernels for heads of up to 64 channels; the next id: up to 128
+    const int of_op = nd.op == NG_OP_ATTENTION ? 0 : dbias ? 4 : nd.op - NG_OP_ATTENTION_DQ + 1;
+    const int waves[2][5] = {{KID_ATTN_W64, KID_ATTN_DQ_W64, KID_ATTN_DK_W64, KID_ATTN_DV_W64, KID_NONE}, {KID_ATTNB_W64, KID_ATTNB_DQ_W64, KID_ATTNB_DK_W64, KID_ATTNB_DV_W64, KID_ATTNB_DB_W64}};
+    const int through_lds[2][5] = {{KID_ATTN_T64, KID_ATTN_DQ_T64, KID_ATTN_DK_T64, KID_ATTN_DV_T64, KID_NONE}, {KID_ATTNB_T64, KID_ATTNB_DQ_T64, KID_ATTNB_DK_T64, KID_ATTNB_DV_T64, KID_ATTNB_DB_T64}};
+    p.kid = waves[biased][of_op] + (narrow ? 0 : 1);
     const long columns = by_keys ? Tk : group * Tq;
     long per_block = 16, other = 64, few = 4;                  // columns of a workgroup, the other side's in a block, blocks a split has at least
     // Straight from memory with 16 columns a wavefront, or 128 columns a workgroup through LDS. The former where there are few
@@ -706,16 +730,16 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     // 64 heads 17.5 / 8.9 (2048); dq 12.4 / 13.3, 11.8 / 13.6, 24.4 / 29.5, 23.5 / 12.3, 19.6 / 12.6. dk and dv share a launch through LDS with up
     // to 64 channels; with more, 128 x 128 with four heads 21 + 15 / 24 + 18 (64), 48 x 512 with 32 heads 49 + 35 / 18 + 13 (1024).
     const long wavefronts = q.n * nd.p.kv_heads * ceil_div(columns, 16) * (by_keys ? group * ceil_div(Tq, 64) : ceil_div(Tk, 64));
-    const bool tiles = !g->unsplit_products && columns > 32 && (wavefronts > 768 || (by_keys && narrow));
-    if (nd.op == NG_OP_ATTENTION && tiles) {
-        p.kid = narrow ? KID_ATTN_T64 : KID_ATTN_T128;
-        per_block = kAttentionColumns, other = narrow ? attention_block<64>() : attention_block<128>(), few = 1;
-    } else if (tiles) {
-        p.kid = nd.op == NG_OP_ATTENTION_DQ ? (narrow ? KID_ATTN_DQ_T64 : KID_ATTN_DQ_T128) : nd.op == NG_OP_ATTENTION_DK ? (narrow ? KID_ATTN_DK_T64 : KID_ATTN_DK_T128)
-              : (narrow ? KID_ATTN_DV_T64 : KID_ATTN_DV_T128);
-        per_block = kAttentionColumns, other = kGradientBlock, few = 1;
+    // With a bias the tile kernels' columns are of one head, which has to have enough of them.
+    const bool by_heads = biased && !by_keys;
+    const bool tiles = !g->unsplit_products && (by_heads ? Tq : columns) > 32 && (wavefronts > 768 || (by_keys && narrow));
+    if (tiles) {
+        p.kid = through_lds[biased][of_op] + (narrow ? 0 : 1);
+        per_block = kAttentionColumns, few = 1;
+        other = nd.op != NG_OP_ATTENTION ? kGradientBlock : narrow ? attention_block<64>() : attention_block<128>();
     }
-    p.col_blocks = (int)ceil_div(columns, per_block);
+    p.query_blocks = (int)ceil_div(Tq, per_block);
+    p.col_blocks = (int)(by_heads && (tiles || dbias) ? group * p.query_blocks : ceil_div(columns, per_block));
     const long groups = q.n * nd.p.kv_heads * p.col_blocks, blocks = by_keys ? group * ceil_div(Tq, other) : ceil_div(Tk, other);
     long want = 1;
     if (per_block == kAttentionColumns)
@@ -726,7 +750,11 @@ AttentionPlan attention_plan(const ng_graph* g, int v) {
     p.per_split = (int)(ceil_div(ceil_div(blocks, want), few) * few);
     p.splits = (int)ceil_div(blocks, p.per_split);
     p.tiles = groups * p.splits;
-    if (p.splits > 1) {
+    if (dbias) {                                               // for each head: rows of sums of its workgroups, and of groups of them
+        const long rows = q.n * p.query_blocks * p.splits, sums = row_groups((int)rows), distances = g->nodes[nd.preds.back()].out.h * g->nodes[nd.preds.back()].out.w;
+        p.ws_floats = (size_t)round64(nd.p.heads * (rows + sums) * ((distances + 3) & ~3L));
+        p.cnt_words = (size_t)round64(nd.p.heads * (1 + sums));
+    } else if (p.splits > 1) {
         p.ws_floats = (size_t)round64(p.tiles * (d + (nd.op == NG_OP_ATTENTION ? 2 : 0)) * per_block);
         p.cnt_words = (size_t)round64(groups);
     }
@@ -1436,17 +1464,23 @@ int build_task(ng_graph* g, int v, char* arena, float* packed, Task& t) {
         case NG_OP_ATTENTION:
         case NG_OP_ATTENTION_DQ:
         case NG_OP_ATTENTION_DK:
-        case NG_OP_ATTENTION_DV: {
+        case NG_OP_ATTENTION_DV:
+        case NG_OP_ATTENTION_DBIAS: {
             const AttentionPlan p = attention_plan(g, v);
             const int first = nd.op == NG_OP_ATTENTION ? 0 : 2;
             const Shape &q = g->nodes[nd.preds[first]].out, &k = g->nodes[nd.preds[first + 1]].out;
             AttnArgs a{};
             a.q = buf(nd.preds[first]), a.k = buf(nd.preds[first + 1]), a.v = buf(nd.preds[first + 2]);
-            if ((int)nd.preds.size() == first + 4) a.len = buf(nd.preds[first + 3]);
+            if ((int)nd.preds.size() == first + 4 + (nd.p.bias != 0)) a.len = buf(nd.preds[first + 3]);
+            if (nd.p.bias != 0) {
+                const Shape& bias = g->nodes[nd.preds.back()].out;
+                a.bias = buf(nd.preds.back()), a.reach = (int)((bias.h * bias.w - 1) / 2), a.from_last = nd.p.bias == 2, a.query_blocks = p.query_blocks;
+            }
             if (first) a.dy = buf(nd.preds[0]), a.rows = buf(nd.preds[1]);
             a.y = buf(v);
             if (p.ws_floats + p.stats_floats > 0 && !packed) return g->fail(NG_EINVAL, "node %d: no workspace", v);
-            if (p.splits > 1) a.ws = packed, a.cnt = reinterpret_cast<unsigned*>(packed + p.ws_floats);
+            if (nd.op == NG_OP_ATTENTION_DBIAS) a.db = buf(v), a.db_ws = packed, a.db_cnt = reinterpret_cast<unsigned*>(packed + p.ws_floats);
+            else if (p.splits > 1) a.ws = packed, a.cnt = reinterpret_cast<unsigned*>(packed + p.ws_floats);
             if (p.stats_floats > 0) a.stats = packed + p.ws_floats + p.cnt_words;
             a.scale = nd.p.scale, a.scale_log2 = (float)((double)nd.p.scale * 1.4426950408889634074);
             a.N = (int)q.n, a.H = nd.p.heads, a.Hk = nd.p.kv_heads, a.d = (int)(q.c / nd.p.heads), a.Tq = (int)(q.h * q.w), a.Tk = (int)(k.h * k.w);

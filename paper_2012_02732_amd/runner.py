@@ -61,7 +61,8 @@ _OPS = {"conv1x1": B.NG_OP_CONV1X1, "dwconv": B.NG_OP_DWCONV, "conv3x3": B.NG_OP
         "attention": B.NG_OP_ATTENTION, "attention_rows": B.NG_OP_ATTENTION_ROWS, "attention_dq": B.NG_OP_ATTENTION_DQ,
         "attention_dk": B.NG_OP_ATTENTION_DK, "attention_dv": B.NG_OP_ATTENTION_DV,
         "layer_norm": B.NG_OP_LAYER_NORM, "layer_norm_dgrad": B.NG_OP_LAYER_NORM_DGRAD, "layer_norm_wgrad": B.NG_OP_LAYER_NORM_WGRAD,
-        "dropout": B.NG_OP_DROPOUT, "position_bias": B.NG_OP_POSITION_BIAS, "position_bias_wgrad": B.NG_OP_POSITION_BIAS_WGRAD}
+        "dropout": B.NG_OP_DROPOUT, "position_bias": B.NG_OP_POSITION_BIAS, "position_bias_wgrad": B.NG_OP_POSITION_BIAS_WGRAD,
+        "attention_dbias": B.NG_OP_ATTENTION_DBIAS}
 
 
 def _params(nd) -> B.ng_op_params:
@@ -81,6 +82,7 @@ def _params(nd) -> B.ng_op_params:
         p.lr, p.slice_lo[0], p.cout = float(q["lr"]), int(q["offset"]), int(q["numel"])
     for name in ("heads", "kv_heads", "rot", "interleaved", "site", "buckets", "max_distance", "both"):
         setattr(p, name, int(q.get(name, 0)))
+    p.bias = {None: 0, "first": 1, "last": 2}[q.get("bias")]
     p.factor, p.scale, p.rate = float(q.get("factor", 1.0)), float(q.get("scale", 0.0)), float(q.get("rate", 0.0))
     return p
 

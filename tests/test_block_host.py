@@ -148,3 +148,32 @@ def test_training_graph_of_a_transformer_block():
         assert ops.count("layer_norm_dgrad") == 3 and ops.count("layer_norm_wgrad") == 4       # nothing below the first norm has a gradient
         assert ops.count("dropout") == 8 and ops.count("attention_dbias") == 2 and ops.count("position_bias_wgrad") == 1
         assert {(v, j) for v, nd in enumerate(w.nodes) for j in range(len(nd.weights))} == set(tw.update_of)
+
+
+def test_biased_attention_shapes_and_refusals():
+    g = G(q=(2, 32, 1, 5), k=(2, 16, 3, 3), ln=(2, 1, 1, 1), bias=(1, 4, 1, 7), even=(1, 4, 1, 6), heads2=(1, 2, 1, 7), tall=(1, 4, 7, 1), each=(2, 4, 1, 7),
+          wide=(1, 4, 1, 2049), dy=(2, 32, 1, 5), one=(1, 4, 1, 1))
+    att, rows_op, db = B.NG_OP_ATTENTION, B.NG_OP_ATTENTION_ROWS, B.NG_OP_ATTENTION_DBIAS
+    how = dict(heads=4, kv_heads=2, scale=0.5, bias=1)
+    y = g.add(att, ["q", "k", "k", "bias"], **how)
+    z = g.add(att, ["q", "k", "k", "ln", "bias"], **dict(how, bias=2))
+    plain = g.add(att, ["q", "k", "k", "ln"], **dict(how, bias=0))
+    assert g.shape(att, ["q", "k", "k", "one"], **how) == (2, 32, 1, 5)
+    rows, rows2, rows0 = (g.add(rows_op, ["dy", v], **how) for v in (y, z, plain))
+    for op, shape in ((B.NG_OP_ATTENTION_DQ, (2, 32, 1, 5)), (B.NG_OP_ATTENTION_DK, (2, 16, 3, 3)), (B.NG_OP_ATTENTION_DV, (2, 16, 3, 3)), (db, (1, 4, 1, 7))):
+        assert g.shape(op, ["dy", rows, "q", "k", "k", "bias"], **how) == shape
+        assert g.shape(op, ["dy", rows2, "q", "k", "k", "ln", "bias"], **dict(how, bias=2)) == shape
+        g.refused(B.NG_EINVAL, "rows are of an attention", op, ["dy", rows2, "q", "k", "k", "ln", "bias"], **how)        # aligned otherwise
+        g.refused(B.NG_EINVAL, "rows are of an attention", op, ["dy", rows0, "q", "k", "k", "bias"], **how)
+        g.refused(B.NG_EINVAL, "attention", op, ["dy", rows, "q", "k", "k"], **how)
+        g.refused(B.NG_EINVAL, "bias in", op, ["dy", rows, "q", "k", "k", "bias"], **dict(how, bias=3))
+    g.refused(B.NG_EINVAL, "no bias", db, ["dy", rows0, "q", "k", "k", "ln"], **dict(how, bias=0))
+    for bad in ("even", "heads2", "tall", "each", "wide", "ln"):
+        g.refused(B.NG_ESHAPE, "the bias must be", att, ["q", "k", "k", bad], **how)
+    g.refused(B.NG_ESHAPE, "lengths", att, ["q", "k", "k", "bias"], **dict(how, bias=0))
+    g.refused(B.NG_ESHAPE, "lengths", att, ["q", "k", "k", "bias", "bias"], **how)
+    for value in (-1, 3):
+        g.refused(B.NG_EINVAL, "bias in", att, ["q", "k", "k", "bias"], **dict(how, bias=value))
+    g.refused(B.NG_EINVAL, "attention takes", att, ["q", "k", "k"], **how)
+    assert B.ng_task_work(g.g, y)[0] == 4 * (320 + 2 * 288 + 320 + 28)
+    B.ng_destroy(g.g)
