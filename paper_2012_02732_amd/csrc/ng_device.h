@@ -62,12 +62,12 @@ enum Kid : int {
     // both gradients of norm and rotation in one launch (launched kernels only)
     KID_ROPE_BOTH_4, KID_ROPE_BOTH_8, KID_ROPE_BOTH_N,
     // layer norm, launched kernels only (the resident kernel with these took 366 s to compile instead of 165): any number of channels,
-    // which come from memory again for each sum (M); workgroups of 1024 threads for many channels (W); dx, the gradients of gamma and
-    // beta, and all of them in one launch
-    KID_NORM_M, KID_NORM_W16,
-    KID_NORM_DX_V8, KID_NORM_DX_V16, KID_NORM_DX_S16, KID_NORM_DX_M, KID_NORM_DX_W16,
-    KID_NORM_DG_V8, KID_NORM_DG_V16, KID_NORM_DG_S16, KID_NORM_DG_M, KID_NORM_DG_W16,
-    KID_NORM_BOTH_V8, KID_NORM_BOTH_V16, KID_NORM_BOTH_S16, KID_NORM_BOTH_M, KID_NORM_BOTH_W16,
+    // which come from memory again for each sum (M); workgroups of 512 (H) or 1024 (W) threads for many channels; dx, the gradients of
+    // gamma and beta, and all of them in one launch
+    KID_NORM_M, KID_NORM_H8, KID_NORM_W8, KID_NORM_W16,
+    KID_NORM_DX_V8, KID_NORM_DX_H8, KID_NORM_DX_W8, KID_NORM_DX_S16, KID_NORM_DX_M,
+    KID_NORM_DG_V8, KID_NORM_DG_H8, KID_NORM_DG_W8, KID_NORM_DG_S16, KID_NORM_DG_M,
+    KID_NORM_BOTH_V8, KID_NORM_BOTH_H8, KID_NORM_BOTH_W8, KID_NORM_BOTH_S16, KID_NORM_BOTH_M,
     // attention with a bias of distances, launched kernels only: as above, and the bias's gradient (DB; DQB: with dq)
     KID_ATTNB_W64, KID_ATTNB_W128, KID_ATTNB_DQ_W64, KID_ATTNB_DQ_W128, KID_ATTNB_DK_W64, KID_ATTNB_DK_W128, KID_ATTNB_DV_W64, KID_ATTNB_DV_W128,
     KID_ATTNB_DB_W64, KID_ATTNB_DB_W128,
@@ -78,7 +78,8 @@ enum Kid : int {
 constexpr bool is_attention_tile_kernel(int kid) { return (kid >= KID_ATTN_T64 && kid <= KID_ATTN_DKV_T64) || (kid >= KID_ATTNB_T64 && kid <= KID_ATTNB_DKV_T64); }
 constexpr bool is_launched_attention_kernel(int kid) { return kid >= KID_ATTN_T64 && kid < KID_COUNT; }
 constexpr bool is_attention_kernel(int kid) { return kid >= KID_ROPE_4 && kid < KID_COUNT; }
-constexpr bool is_wide_norm(int kid) { return kid == KID_NORM_W16 || kid == KID_NORM_DX_W16 || kid == KID_NORM_DG_W16 || kid == KID_NORM_BOTH_W16; }
+constexpr bool is_half_norm(int kid) { return kid == KID_NORM_H8 || kid == KID_NORM_DX_H8 || kid == KID_NORM_DG_H8 || kid == KID_NORM_BOTH_H8; }
+constexpr bool is_wide_norm(int kid) { return kid == KID_NORM_W8 || kid == KID_NORM_W16 || kid == KID_NORM_DX_W8 || kid == KID_NORM_DG_W8 || kid == KID_NORM_BOTH_W8; }
 constexpr bool is_train_kernel(int kid) { return kid >= KID_GEMM_PW_FWD && kid <= KID_SGD; }
 
 // the variant without / with a fused add_n of a kernel (ids without such a variant map to themselves / KID_NONE)
@@ -157,7 +158,7 @@ constexpr bool in_build(int build, int kid) {
 }
 
 constexpr int kBlock = 256;          // threads that work on one tile (a stand-alone kernel's workgroup)
-constexpr int block_threads(int kid) { return is_wide_norm(kid) ? 1024 : kBlock; }      // (kernels that are only launched may have more)
+constexpr int block_threads(int kid) { return is_wide_norm(kid) ? 1024 : is_half_norm(kid) ? 512 : kBlock; }      // (kernels that are only launched may have more)
 constexpr int kSubs = 2;             // tiles a workgroup of the resident kernel works on at a time
 constexpr int kGroup = kBlock * kSubs;  // threads per workgroup of the resident kernel
 constexpr int kArgBytes = 256;       // size of the per-task argument block of the resident kernel's task table

@@ -235,10 +235,10 @@ static int pair_kid(const Task& first, const Task& second) {
     if (kid_first == KID_ROPE_DX_8 && kid_second == KID_ROPE_DG_8) return KID_ROPE_BOTH_8;
     if (kid_first == KID_ROPE_DX_N && kid_second == KID_ROPE_DG_N) return KID_ROPE_BOTH_N;
     if (kid_first == KID_NORM_DX_V8 && kid_second == KID_NORM_DG_V8) return KID_NORM_BOTH_V8;
-    if (kid_first == KID_NORM_DX_V16 && kid_second == KID_NORM_DG_V16) return KID_NORM_BOTH_V16;
+    if (kid_first == KID_NORM_DX_H8 && kid_second == KID_NORM_DG_H8) return KID_NORM_BOTH_H8;
     if (kid_first == KID_NORM_DX_S16 && kid_second == KID_NORM_DG_S16) return KID_NORM_BOTH_S16;
     if (kid_first == KID_NORM_DX_M && kid_second == KID_NORM_DG_M) return KID_NORM_BOTH_M;
-    if (kid_first == KID_NORM_DX_W16 && kid_second == KID_NORM_DG_W16) return KID_NORM_BOTH_W16;
+    if (kid_first == KID_NORM_DX_W8 && kid_second == KID_NORM_DG_W8) return KID_NORM_BOTH_W8;
     return KID_NONE;
 }
 bool can_pair(const Task& first, const Task& second) {
@@ -326,10 +326,10 @@ void make_pair_task(const Task& first, const Task& second, Task& t) {
         case KID_ROPE_BOTH_8: set_norm_backward<KID_ROPE_BOTH_8>(first, second, t); break;
         case KID_ROPE_BOTH_N: set_norm_backward<KID_ROPE_BOTH_N>(first, second, t); break;
         case KID_NORM_BOTH_V8: set_norm_backward<KID_NORM_BOTH_V8>(first, second, t); break;
-        case KID_NORM_BOTH_V16: set_norm_backward<KID_NORM_BOTH_V16>(first, second, t); break;
+        case KID_NORM_BOTH_H8: set_norm_backward<KID_NORM_BOTH_H8>(first, second, t); break;
         case KID_NORM_BOTH_S16: set_norm_backward<KID_NORM_BOTH_S16>(first, second, t); break;
         case KID_NORM_BOTH_M: set_norm_backward<KID_NORM_BOTH_M>(first, second, t); break;
-        case KID_NORM_BOTH_W16: set_norm_backward<KID_NORM_BOTH_W16>(first, second, t); break;
+        case KID_NORM_BOTH_W8: set_norm_backward<KID_NORM_BOTH_W8>(first, second, t); break;
         default: t = first; break;
     }
 }
@@ -818,8 +818,8 @@ NormPlan norm_plan(const ng_graph* g, int v) {
     const Shape& x = g->nodes[nd.preds[which ? 1 : 0]].out;
     const long C = x.c, T = x.h * x.w;
     const bool wgrad = nd.op == NG_OP_LAYER_NORM_WGRAD;
+    long most = 512;                                           // workgroups of wgrad
     auto one_of = [which](int forward, int dgrad, int wgrad) { return which == 0 ? forward : which == 1 ? dgrad : wgrad; };
-    const long quads = T >= 4 ? 4 : 1;
     if (C > 4096 || (T < 4 && C * T > 4096)) {
         p.kid = one_of(KID_NORM_M, KID_NORM_DX_M, KID_NORM_DG_M);
         while (p.lanes_log2 < 4 && (1L << p.lanes_log2) < T) ++p.lanes_log2;
@@ -827,17 +827,33 @@ NormPlan norm_plan(const ng_graph* g, int v) {
     } else if (T < 4) {
         p.kid = one_of(KID_NORM_S16, KID_NORM_DX_S16, KID_NORM_DG_S16);
         p.lanes_log2 = T == 1 ? 0 : T == 2 ? 1 : 2;
-    } else if (C > 1024 && x.n * ceil_div(T, 16) >= 256) {
-        p.kid = one_of(KID_NORM_W16, KID_NORM_DX_W16, KID_NORM_DG_W16);
-        p.lanes_log2 = 2;
-        p.blocks = (int)ceil_div(T, 16);
     } else {
-        while (p.lanes_log2 < 3 && C * (2L << p.lanes_log2) <= 4096 && (quads << p.lanes_log2) < T) ++p.lanes_log2;
-        p.kid = C * (1L << p.lanes_log2) <= 8 * kBlock ? one_of(KID_NORM_V8, KID_NORM_DX_V8, KID_NORM_DG_V8) : one_of(KID_NORM_V16, KID_NORM_DX_V16, KID_NORM_DG_V16);
-        p.blocks = (int)ceil_div(T, quads << p.lanes_log2);
+        // Threads side by side along the tokens: as many as leave a workgroup for each compute unit, since what a workgroup reads of a channel
+        // should be whole lines of memory. TB/s of the forward kernel with 2 / 4 / 8 of them, 16 images of 512 channels, 8192 tokens 3.2 / 4.1 / 5.1, of
+        // 1024 channels, 4096 tokens 2.9 / 3.9 / 4.4; both gradients in one launch 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9. Eight take 512 threads for more than 256
+        // channels, 1024 for more than 512, in fewer and larger workgroups: slower where the tensors come out of the 256 MB cache behind the
+        // L2s (8 images of 1024 channels, 4096 tokens 4: 39 us, 8: 54), so only for larger ones. (The gradients of 513 - 1024 channels
+        // gain either way, 121 -> 115.)
+        const bool large = (double)x.elems() * 4 * (which == 0 ? 2 : 3) > 268435456.0;
+        long threads = 0;
+        for (int log2 = 3; log2 >= 0; --log2) {
+            const long lanes = 1L << log2;
+            threads = ceil_div(C * lanes, 8);
+            const bool wide = which == 0 && log2 == 2 && threads > 1024;       // 16 channels a thread
+            if (log2 > 0 && (2 * lanes >= T || (threads > 1024 && !wide) || x.n * ceil_div(T, 4 * lanes) < 256)) continue;
+            if (log2 == 3 && threads > kBlock && !large && !(which > 0 && C > 512)) continue;
+            p.lanes_log2 = log2;
+            break;
+        }
+        p.kid = threads <= kBlock ? one_of(KID_NORM_V8, KID_NORM_DX_V8, KID_NORM_DG_V8)
+              : which == 0 && p.lanes_log2 == 0 ? (int)KID_NORM_V16            // few tokens: a kernel that the device-resident replay has as well
+              : threads <= 512 ? one_of(KID_NORM_H8, KID_NORM_DX_H8, KID_NORM_DG_H8)
+              : threads <= 1024 ? one_of(KID_NORM_W8, KID_NORM_DX_W8, KID_NORM_DG_W8) : (int)KID_NORM_W16;
+        p.blocks = (int)ceil_div(T, 4L << p.lanes_log2);
+        if (p.kid != KID_NORM_DG_V8) most = 256;                // one workgroup of so many threads and registers on a compute unit, all of them at once
     }
     p.items = (int)(x.n * p.blocks);
-    p.per_tile = (int)ceil_div(p.items, wgrad ? 512 : 1L << 20);       // every workgroup of wgrad's leaves a row of sums that somebody has to add up
+    p.per_tile = (int)ceil_div(p.items, wgrad ? most : 1L << 20);      // every workgroup of wgrad's leaves a row of sums that somebody has to add up
     p.tiles = ceil_div(p.items, p.per_tile);
     if (wgrad) {
         p.ws_floats = (size_t)round64((p.tiles + row_groups((int)p.tiles)) * ((2 * C + 3) & ~3L));

@@ -110,22 +110,24 @@ def test_work_of_the_block_operators():
     B.ng_destroy(g.g)
 
 
-NORM_KERNELS = [                # n, c, h, w, name of the forward kernel
-    (8, 1024, 1, 1, "layer_norm_few"), (2, 7, 1, 3, "layer_norm_few"), (1, 2000, 1, 3, "layer_norm_many"), (1, 4097, 1, 1, "layer_norm_many"), (2, 5000, 1, 18, "layer_norm_many"),
-    (6, 520, 1, 333, "layer_norm_16"), (2, 33, 3, 7, "layer_norm_8"), (1, 2048, 2, 8, "layer_norm_16"), (16, 1100, 1, 300, "layer_norm_wide"), (2, 4096, 1, 8192, "layer_norm_wide"),
+NORM_KERNELS = [                # n, c, h, w, name of the forward kernel, what the gradients' end in
+    (8, 1024, 1, 1, "layer_norm_few", "few"), (2, 7, 1, 3, "layer_norm_few", "few"), (1, 2000, 1, 3, "layer_norm_many", "many"), (1, 4097, 1, 1, "layer_norm_many", "many"),
+    (2, 5000, 1, 18, "layer_norm_many", "many"), (6, 520, 1, 333, "layer_norm_8", "8"), (2, 33, 3, 7, "layer_norm_8", "8"), (1, 2048, 2, 8, "layer_norm_8", "8"),
+    (1, 4096, 1, 4, "layer_norm_16", "half"), (16, 600, 1, 259, "layer_norm_half", "half"), (16, 1100, 1, 300, "layer_norm_wide", "wide"), (16, 2100, 1, 259, "layer_norm_wide_16", "wide"),
+    (2, 4096, 1, 8192, "layer_norm_wide_16", "wide"), (8, 1024, 1, 4096, "layer_norm_half", "wide"), (16, 1024, 1, 4096, "layer_norm_wide", "wide"), (16, 512, 1, 8192, "layer_norm_half", "half"),
 ]
 
 
 @pytest.mark.parametrize("case", NORM_KERNELS, ids=str)
 def test_kernels_of_layer_norm(case):
-    n, c, h, w, name = case
+    n, c, h, w, name, gradients = case
     x = np.broadcast_to(np.float32(0), (n, c, h, w))
     g = norm_graph(np.zeros((1, 1, 1, 1), np.float32), np.zeros(1, np.float32), np.zeros(1, np.float32), np.zeros((1, 1, 1, 1), np.float32), 1e-5)
     for nd in g.nodes[:1] + [g.nodes[g.names["dy"]]]:           # the shapes alone
         nd.params = dict(zip("nchw", x.shape))
     found = kernels(g)
     assert found["y"] == name
-    assert found["dx"] == name.replace("layer_norm", "layer_norm_dgrad") and found["dw"] == name.replace("layer_norm", "layer_norm_wgrad")
+    assert found["dx"] == f"layer_norm_dgrad_{gradients}" and found["dw"] == f"layer_norm_wgrad_{gradients}"
 
 
 def test_gradients_of_a_norm_share_a_launch():

@@ -23,7 +23,7 @@ def norm_inputs(seed, n, c, h, w, offset=0.5):
 NORM = [                        # n, c, h, w
     (1, 1, 1, 1), (1, 1, 2, 9), (2, 3, 1, 2), (3, 5, 1, 3), (2, 7, 1, 5), (1, 64, 1, 4), (8, 1024, 1, 1), (5, 1023, 1, 1), (2, 1300, 1, 2), (2, 257, 3, 7), (1, 600, 1, 17), (4, 96, 1, 31),
     (2, 1025, 1, 33), (1, 2048, 2, 8), (1, 4096, 1, 9), (3, 2047, 1, 3), (1, 4097, 1, 3), (2, 5000, 1, 18), (1, 9001, 1, 1), (16, 1100, 1, 259), (130, 4, 1, 37), (700, 40, 1, 6),
-    (513, 33, 1, 1), (6, 520, 1, 333),
+    (513, 33, 1, 1), (6, 520, 1, 333), (16, 600, 1, 259), (17, 2100, 1, 255), (40, 700, 1, 300), (3, 3000, 1, 350), (33, 200, 1, 260), (2, 1, 1, 9001),
 ]
 
 
@@ -60,6 +60,30 @@ def test_layer_norm_of_a_large_mean_and_of_equal_channels():
     got = run(norm_graph(flat, gamma, beta, dy, 1e-5))[B.NG_MODE_GRAPH_SINGLE]
     assert np.array_equal(got["y"], np.broadcast_to(beta[None, :, None, None], x.shape))
     within(got, norm_reference(flat, gamma, beta, dy, 1e-5), "equal channels")
+
+
+def test_layer_norm_of_tensors_beyond_the_caches():
+    """The kernels that only large tensors get, against torch in 64 bits on the GPU: 2-norms within the roundings of the formula (mean and
+    variance 22 u, three products, a sum over 60001 tokens in parts of 240: sqrt u)."""
+    for n, c, t in ((2, 300, 60001), (2, 700, 30003), (1, 3100, 12005)):
+        g = torch.Generator("cuda:0").manual_seed(c)
+        x, dy = (torch.randn(n, c, 1, t, generator=g, device="cuda:0") for _ in range(2))
+        gamma, beta = (torch.randn(c, generator=g, device="cuda:0") for _ in range(2))
+        graph = norm_graph(np.zeros((1, 1, 1, 1), F32), gamma.cpu().numpy(), beta.cpu().numpy(), np.zeros((1, 1, 1, 1), F32), 1e-5)
+        for name, value in (("x", x), ("dy", dy)):
+            graph.nodes[graph.names[name]].params = dict(n=n, c=c, h=1, w=t)
+            graph.inputs[graph.names[name]] = value
+        r = GraphRunner(graph.workload(), "cuda:0")
+        r.prepare(plan_trials=1)
+        r.replay(B.NG_MODE_GRAPH_SINGLE)
+        r.sync()
+        leaves = [v.double().requires_grad_() for v in (x, gamma, beta)]
+        y = torch.nn.functional.layer_norm(leaves[0].transpose(1, 3), (c,), leaves[1], leaves[2], 1e-5).transpose(1, 3)
+        dx, dg, db = torch.autograd.grad(y, leaves, dy.double())
+        for name, ref in (("y", y.detach()), ("dx", dx), ("dw", torch.stack([dg, db]).view(2, c, 1, 1))):
+            off = float((r.tensor(graph.names[name]).double() - ref).norm() / ref.norm())
+            assert off <= 40 * U, (c, name, off / U)
+        r.close()
 
 
 def test_layer_norm_keeps_tokens_apart():
