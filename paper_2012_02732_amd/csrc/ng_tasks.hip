@@ -828,7 +828,9 @@ NormPlan norm_plan(const ng_graph* g, int v) {
         p.kid = one_of(KID_NORM_S16, KID_NORM_DX_S16, KID_NORM_DG_S16);
         p.lanes_log2 = T == 1 ? 0 : T == 2 ? 1 : 2;
     } else {
-        // Threads side by side along the tokens: as many as leave a workgroup for each compute unit, since what a workgroup reads of a channel
+        // Threads side by side along the tokens: as many as leave 64 workgroups, 128 of more than 256 threads (few workgroups have few rows of sums to
+        // join: forward and both gradients of 4 images of 256 channels, 400 tokens with at least 64 / 128 / 256 workgroups 15.4 / 16.8 / 19.5 us, of 6
+        // images of 520 channels, 333 tokens, where 64 are of 1024 threads, 27.0 / 21.6 / 24.9), since what a workgroup reads of a channel
         // should be whole lines of memory. TB/s of the forward kernel with 2 / 4 / 8 of them, 16 images of 512 channels, 8192 tokens 3.2 / 4.1 / 5.1, of
         // 1024 channels, 4096 tokens 2.9 / 3.9 / 4.4; both gradients in one launch 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9. Eight take 512 threads for more than 256
         // channels, 1024 for more than 512, in fewer and larger workgroups: slower where the tensors come out of the 256 MB cache behind the
@@ -840,7 +842,7 @@ NormPlan norm_plan(const ng_graph* g, int v) {
             const long lanes = 1L << log2;
             threads = ceil_div(C * lanes, 8);
             const bool wide = which == 0 && log2 == 2 && threads > 1024;       // 16 channels a thread
-            if (log2 > 0 && (2 * lanes >= T || (threads > 1024 && !wide) || x.n * ceil_div(T, 4 * lanes) < 256)) continue;
+            if (log2 > 0 && (2 * lanes >= T || (threads > 1024 && !wide) || x.n * ceil_div(T, 4 * lanes) < (threads <= kBlock ? 64 : 128))) continue;
             if (log2 == 3 && threads > kBlock && !large && !(which > 0 && C > 512)) continue;
             p.lanes_log2 = log2;
             break;
