@@ -2036,7 +2036,7 @@ NG_KERNEL(KID_NORM_V16, NormArgs, "layer_norm_16", norm_tile < NORM_FWD, 256, 4,
 NG_KERNEL(KID_NORM_S16, NormArgs, "layer_norm_few", norm_tile < NORM_FWD, 256, 1, 16)
 NG_KERNEL(KID_NORM_M, NormArgs, "layer_norm_many", norm_many_tile < NORM_FWD)
 NG_KERNEL(KID_NORM_H8, NormArgs, "layer_norm_half", norm_tile < NORM_FWD, 512, 4, 8)
-NG_KERNEL(KID_NORM_W8, NormArgs, "layer_norm_wide", norm_tile < NORM_FWD, 1024, 4, 8)
+NG_KERNEL(KID_NORM_H16, NormArgs, "layer_norm_half_16", norm_tile < NORM_FWD, 512, 4, 16)
 NG_KERNEL(KID_NORM_W16, NormArgs, "layer_norm_wide_16", norm_tile < NORM_FWD, 1024, 4, 16)
 NG_KERNEL(KID_NORM_DX_V8, NormArgs, "layer_norm_dgrad_8", norm_tile < NORM_DX, 256, 4, 8)
 NG_KERNEL(KID_NORM_DX_H8, NormArgs, "layer_norm_dgrad_half", norm_tile < NORM_DX, 512, 4, 8)
@@ -2106,7 +2106,7 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_ATTN_DV_W64) X(KID_ATTN_DV_W128) X(KID_ATTN_T64) X(KID_ATTN_T128) X(KID_ATTN_DQ_T64) X(KID_ATTN_DQ_T128)    \
     X(KID_ATTN_DK_T64) X(KID_ATTN_DK_T128) X(KID_ATTN_DV_T64) X(KID_ATTN_DV_T128)    \
     X(KID_ATTN_DKV_T64) X(KID_ROPE_BOTH_4) X(KID_ROPE_BOTH_8) X(KID_ROPE_BOTH_N)    \
-    X(KID_NORM_V8) X(KID_NORM_V16) X(KID_NORM_S16) X(KID_NORM_M) X(KID_NORM_H8) X(KID_NORM_W8) X(KID_NORM_W16)    \
+    X(KID_NORM_V8) X(KID_NORM_V16) X(KID_NORM_S16) X(KID_NORM_M) X(KID_NORM_H8) X(KID_NORM_H16) X(KID_NORM_W16)    \
     X(KID_NORM_DX_V8) X(KID_NORM_DX_H8) X(KID_NORM_DX_S16) X(KID_NORM_DX_M) X(KID_NORM_DX_W8)    \
     X(KID_NORM_DG_V8) X(KID_NORM_DG_H8) X(KID_NORM_DG_S16) X(KID_NORM_DG_M) X(KID_NORM_DG_W8)    \
     X(KID_NORM_BOTH_V8) X(KID_NORM_BOTH_H8) X(KID_NORM_BOTH_S16) X(KID_NORM_BOTH_M) X(KID_NORM_BOTH_W8)    \

@@ -828,21 +828,22 @@ NormPlan norm_plan(const ng_graph* g, int v) {
         p.kid = one_of(KID_NORM_S16, KID_NORM_DX_S16, KID_NORM_DG_S16);
         p.lanes_log2 = T == 1 ? 0 : T == 2 ? 1 : 2;
     } else {
-        // Threads side by side along the tokens: as many as leave 64 workgroups, 128 of more than 256 threads (few workgroups have few rows of sums to
-        // join: forward and both gradients of 4 images of 256 channels, 400 tokens with at least 64 / 128 / 256 workgroups 15.4 / 16.8 / 19.5 us, of 6
-        // images of 520 channels, 333 tokens, where 64 are of 1024 threads, 27.0 / 21.6 / 24.9), since what a workgroup reads of a channel
-        // should be whole lines of memory. TB/s of the forward kernel with 2 / 4 / 8 of them, 16 images of 512 channels, 8192 tokens 3.2 / 4.1 / 5.1, of
-        // 1024 channels, 4096 tokens 2.9 / 3.9 / 4.4; both gradients in one launch 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9. Eight take 512 threads for more than 256
-        // channels, 1024 for more than 512, in fewer and larger workgroups: slower where the tensors come out of the 256 MB cache behind the
-        // L2s (8 images of 1024 channels, 4096 tokens 4: 39 us, 8: 54), so only for larger ones. (The gradients of 513 - 1024 channels
-        // gain either way, 121 -> 115.)
+        // Threads side by side along the tokens: as many as leave 64 workgroups, 128 of more than 256 threads, 256 of more than 512 (few workgroups have few
+        // rows of sums to join: forward and both gradients of 4 images of 256 channels, 400 tokens with at least 64 / 128 / 256 workgroups 15.4 /
+        // 16.8 / 19.5 us, of 6 images of 520 channels, 333 tokens, where 64 are of 1024 threads, 27.0 / 21.6 / 24.9; both gradients of 16
+        // images of 1000 channels, 300 tokens in 160 of 1024 threads 29.3, in twice as many of 512 26.2), since what a workgroup reads of a channel
+        // should be whole lines of memory. TB/s of the forward kernel with 2 / 4 / 8 of them, 16 images of 512 channels, 8192 tokens 3.3 / 4.1 / 5.1, of
+        // 1024 channels, 4096 tokens 2.9 / 3.9 / 4.8; both gradients in one launch 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9. Eight take 512 threads for more than 256
+        // channels, 1024 for more than 512 (forward: 1024), in fewer and larger workgroups: not faster where the tensors come out of the 256 MB cache
+        // behind the L2s (4 images of 2048 channels, 4096 tokens 4: 44 us, 8: 51), so only for larger ones. (The gradients of 513 - 1024 channels
+        // gain either way, 121 -> 115.) A forward kernel of 512 threads with 16 channels each takes the place of 1024 with 8: 123 -> 113 us and, in
+        // the cache, 53 -> 39 (16 and 8 images of 1024 channels, 4096 tokens, 8 side by side).
         const bool large = (double)x.elems() * 4 * (which == 0 ? 2 : 3) > 268435456.0;
         long threads = 0;
         for (int log2 = 3; log2 >= 0; --log2) {
             const long lanes = 1L << log2;
             threads = ceil_div(C * lanes, 8);
-            const bool wide = which == 0 && log2 == 2 && threads > 1024;       // 16 channels a thread
-            if (log2 > 0 && (2 * lanes >= T || (threads > 1024 && !wide) || x.n * ceil_div(T, 4 * lanes) < (threads <= kBlock ? 64 : 128))) continue;
+            if (log2 > 0 && (2 * lanes >= T || threads > (which == 0 ? 2048 : 1024) || x.n * ceil_div(T, 4 * lanes) < (threads <= kBlock ? 64 : threads <= 512 ? 128 : 256))) continue;
             if (log2 == 3 && threads > kBlock && !large && !(which > 0 && C > 512)) continue;
             p.lanes_log2 = log2;
             break;
@@ -850,7 +851,7 @@ NormPlan norm_plan(const ng_graph* g, int v) {
         p.kid = threads <= kBlock ? one_of(KID_NORM_V8, KID_NORM_DX_V8, KID_NORM_DG_V8)
               : which == 0 && p.lanes_log2 == 0 ? (int)KID_NORM_V16            // few tokens: a kernel that the device-resident replay has as well
               : threads <= 512 ? one_of(KID_NORM_H8, KID_NORM_DX_H8, KID_NORM_DG_H8)
-              : threads <= 1024 ? one_of(KID_NORM_W8, KID_NORM_DX_W8, KID_NORM_DG_W8) : (int)KID_NORM_W16;
+              : threads <= 1024 ? one_of(KID_NORM_H16, KID_NORM_DX_W8, KID_NORM_DG_W8) : (int)KID_NORM_W16;      // (16 channels a thread)
         p.blocks = (int)ceil_div(T, 4L << p.lanes_log2);
         if (p.kid != KID_NORM_DG_V8) most = 256;                // one workgroup of so many threads and registers on a compute unit, all of them at once
     }

@@ -86,7 +86,7 @@ def norm_reference(x, gamma, beta, dy, eps):
         off2 = (S + 3) * U * np.abs(u * xh).mean(1, keepdims=True) + (np.abs(u) * e_xh).mean(1, keepdims=True)
         inside = 3 * U * np.abs(u) + off1 + 3 * U * np.abs(m1) + np.abs(xh) * off2 + np.abs(m2) * e_xh + 4 * U * np.abs(xh * m2)
         out["dx"] = dx, (inside + (off_r + 3 * U) * (np.abs(u) + np.abs(m1) + np.abs(xh * m2))) / s
-        # over P tokens: 256 workgroups at least where there are enough, so 4 ceil(P / 256) terms of a thread, then 8 + 16 + 32 sums of sums (fewer
+        # over P tokens: a thread walks at most ceil(P / 1024) blocks of four, within 4 ceil(P / 256) terms, then 8 + 16 + 32 sums of sums (fewer
         # where there are fewer tokens)
         P = x.size // c
         D = min(P, 4 * (P // 256 + 1) + 60) + 2

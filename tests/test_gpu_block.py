@@ -65,7 +65,7 @@ def test_layer_norm_of_a_large_mean_and_of_equal_channels():
 def test_layer_norm_of_tensors_beyond_the_caches():
     """The kernels that only large tensors get, against torch in 64 bits on the GPU: 2-norms within the roundings of the formula (mean and
     variance 22 u, three products, a sum over 60001 tokens in parts of 240: sqrt u)."""
-    for n, c, t in ((2, 300, 60001), (2, 700, 30003), (1, 3100, 12005)):
+    for n, c, t in ((2, 300, 60001), (2, 700, 30003), (1, 3100, 12005), (9, 1000, 3751), (5, 1900, 3606)):
         g = torch.Generator("cuda:0").manual_seed(c)
         x, dy = (torch.randn(n, c, 1, t, generator=g, device="cuda:0") for _ in range(2))
         gamma, beta = (torch.randn(c, generator=g, device="cuda:0") for _ in range(2))
