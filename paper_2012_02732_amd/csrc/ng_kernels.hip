@@ -2075,7 +2075,6 @@ NG_KERNEL(KID_ATTNB_DB_T64, AttnArgs, "attention_dbias_tile_64", attention_dq_ti
 NG_KERNEL(KID_ATTNB_DQB_T64, AttnArgs, "attention_biased_dq+dbias_tile_64", attention_dq_tile < 64, true, true, true)
 NG_KERNEL(KID_ATTNB_DB_W128, AttnArgs, "attention_dbias_wave_128", attention_dbias_wave_tile < 8)
 NG_KERNEL(KID_ATTNB_DB_T128, AttnArgs, "attention_dbias_tile_128", attention_dq_tile < 128, false, true, true)
-NG_KERNEL(KID_ATTNB_DQB_T128, AttnArgs, "attention_biased_dq+dbias_tile_128", attention_dq_tile < 128, true, true, true)
 #undef NG_KERNEL
 NG_KERNEL0(KID_ATTN_ROWS, AttnArgs, "attention_rows", attention_rows_tile)
 NG_KERNEL0(KID_DROPOUT, DropoutArgs, "dropout", dropout_tile)
@@ -2114,7 +2113,7 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_ATTNB_W64) X(KID_ATTNB_W128) X(KID_ATTNB_DQ_W64) X(KID_ATTNB_DQ_W128) X(KID_ATTNB_DK_W64) X(KID_ATTNB_DK_W128)    \
     X(KID_ATTNB_DV_W64) X(KID_ATTNB_DV_W128) X(KID_ATTNB_T64) X(KID_ATTNB_T128) X(KID_ATTNB_DQ_T64) X(KID_ATTNB_DQ_T128)    \
     X(KID_ATTNB_DK_T64) X(KID_ATTNB_DK_T128) X(KID_ATTNB_DV_T64) X(KID_ATTNB_DV_T128) X(KID_ATTNB_DKV_T64) X(KID_ATTNB_DB_W64)    \
-    X(KID_ATTNB_DB_T64) X(KID_ATTNB_DQB_T64) X(KID_ATTNB_DB_W128) X(KID_ATTNB_DB_T128) X(KID_ATTNB_DQB_T128)
+    X(KID_ATTNB_DB_T64) X(KID_ATTNB_DQB_T64) X(KID_ATTNB_DB_W128) X(KID_ATTNB_DB_T128)
 
 // A batch-norm epilogue is written into a task's argument block by type (C3Args or PwArgs, whose `ep` fields sit at
 // different offsets): the predicates that name the type must agree with the type the kernel takes.

@@ -230,7 +230,6 @@ static int pair_kid(const Task& first, const Task& second) {
     if (kid_first == KID_ATTN_DK_T64 && kid_second == KID_ATTN_DV_T64) return KID_ATTN_DKV_T64;
     if (kid_first == KID_ATTNB_DK_T64 && kid_second == KID_ATTNB_DV_T64) return KID_ATTNB_DKV_T64;
     if (kid_first == KID_ATTNB_DQ_T64 && kid_second == KID_ATTNB_DB_T64) return KID_ATTNB_DQB_T64;
-    if (kid_first == KID_ATTNB_DQ_T128 && kid_second == KID_ATTNB_DB_T128) return KID_ATTNB_DQB_T128;
     if (kid_first == KID_ROPE_DX_4 && kid_second == KID_ROPE_DG_4) return KID_ROPE_BOTH_4;
     if (kid_first == KID_ROPE_DX_8 && kid_second == KID_ROPE_DG_8) return KID_ROPE_BOTH_8;
     if (kid_first == KID_ROPE_DX_N && kid_second == KID_ROPE_DG_N) return KID_ROPE_BOTH_N;
@@ -321,7 +320,6 @@ void make_pair_task(const Task& first, const Task& second, Task& t) {
             t.ntiles = first.ntiles, t.grid[0] = (unsigned)first.ntiles;
             break;
         case KID_ATTNB_DQB_T64: set_dq_dbias<KID_ATTNB_DQB_T64>(first, second, t); break;
-        case KID_ATTNB_DQB_T128: set_dq_dbias<KID_ATTNB_DQB_T128>(first, second, t); break;
         case KID_ROPE_BOTH_4: set_norm_backward<KID_ROPE_BOTH_4>(first, second, t); break;
         case KID_ROPE_BOTH_8: set_norm_backward<KID_ROPE_BOTH_8>(first, second, t); break;
         case KID_ROPE_BOTH_N: set_norm_backward<KID_ROPE_BOTH_N>(first, second, t); break;
