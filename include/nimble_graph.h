@@ -275,7 +275,7 @@ int ng_set_memory_reuse(ng_graph* g, int on);
  * and x) are computed in one walk over dy and x by the launch of whichever of the two comes first, if
  * both are on one stream (always, in modes 1 and 2); likewise the input gradient and the weight gradient
  * of a depthwise or 1 x 1 convolution (same dy) share one launch, their workgroups interleaved, if
- * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, those of NG_OP_LAYER_NORM, dq and the bias's gradient of an attention with many queries, and dk and
+ * everything the later one reads is complete when the earlier one starts; likewise the two gradients of NG_OP_HEAD_ROPE, those of NG_OP_LAYER_NORM, dq and the bias's gradient of an attention with many queries and heads of up to 64 channels, and dk and
  * dv of an attention with many keys and heads of up to 64 channels, with what both need computed once. In modes 1 and 2 tasks of the
  * same kernel that do not wait for each other share a launch as well, and the launches follow each other in an
  * order that lets them (ng_get_single_launches; attention operators' kernels have a launch each). on = 0 switches the exceptions off: one kernel per task. Call before ng_bind (NG_ESTATE after). */

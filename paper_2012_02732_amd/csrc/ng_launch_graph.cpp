@@ -32,7 +32,7 @@ static bool same_attention(const ng_op_params& a, const ng_op_params& b) {
 //     for an update: it already comes after every reader of its weights, and it keeps its place in the stream, so
 //     the last one's launch comes after everything the earlier ones waited for;
 //   * the input gradient and gamma's gradient of a norm and rotation of heads, those of a layer norm, dk and dv of an attention with heads of up to 64
-//     channels, and dq of an attention with many queries and its bias's gradient, likewise share a launch with the work that both need done once;
+//     channels, and dq of such an attention with many queries and its bias's gradient, likewise share a launch with the work that both need done once;
 //   * the input gradient and the parameter gradients of a batch-norm (same dy, same x) are computed by one launch, at
 //     the place of whichever of the two tasks comes first on their stream (fused_into[the later one] = the earlier
 //     one). Both are ready when the first one is (same inputs), each tensor has its buffer to itself, and the later
