@@ -833,8 +833,8 @@ NormPlan norm_plan(const ng_graph* g, int v) {
         // should be whole lines of memory. TB/s of the forward kernel with 2 / 4 / 8 of them, 16 images of 512 channels, 8192 tokens 3.3 / 4.1 / 5.1, of
         // 1024 channels, 4096 tokens 2.9 / 3.9 / 4.8; both gradients in one launch 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9. Eight take 512 threads for more than 256
         // channels, 1024 for more than 512 (forward: 1024), in fewer and larger workgroups: not faster where the tensors come out of the 256 MB cache
-        // behind the L2s (4 images of 2048 channels, 4096 tokens 4: 44 us, 8: 51), so only for larger ones. (The gradients of 513 - 1024 channels
-        // gain either way, 121 -> 115.) A forward kernel of 512 threads with 16 channels each takes the place of 1024 with 8: 123 -> 113 us and, in
+        // behind the L2s (4 images of 2048 channels, 4096 tokens 4: 44 us, 8: 51), so only for larger ones (both gradients of 8
+        // images of 1024 channels, 4096 tokens, 400 MB, 4: 121, 8: 115; of 2048 tokens 49 and 58). A forward kernel of 512 threads with 16 channels each takes the place of 1024 with 8: 123 -> 113 us and, in
         // the cache, 53 -> 39 (16 and 8 images of 1024 channels, 4096 tokens, 8 side by side).
         const bool large = (double)x.elems() * 4 * (which == 0 ? 2 : 3) > 268435456.0;
         long threads = 0;
@@ -842,7 +842,7 @@ NormPlan norm_plan(const ng_graph* g, int v) {
             const long lanes = 1L << log2;
             threads = ceil_div(C * lanes, 8);
             if (log2 > 0 && (2 * lanes >= T || threads > (which == 0 ? 2048 : 1024) || x.n * ceil_div(T, 4 * lanes) < (threads <= kBlock ? 64 : threads <= 512 ? 128 : 256))) continue;
-            if (log2 == 3 && threads > kBlock && !large && !(which > 0 && C > 512)) continue;
+            if (log2 == 3 && threads > kBlock && !large) continue;
             p.lanes_log2 = log2;
             break;
         }
