@@ -65,9 +65,9 @@ enum Kid : int {
     // which come from memory again for each sum (M); workgroups of 512 (H) or 1024 (W) threads for many channels; dx, the gradients of
     // gamma and beta, and all of them in one launch
     KID_NORM_M, KID_NORM_H8, KID_NORM_H16, KID_NORM_W16,
-    KID_NORM_DX_V8, KID_NORM_DX_H8, KID_NORM_DX_W8, KID_NORM_DX_S16, KID_NORM_DX_M,
-    KID_NORM_DG_V8, KID_NORM_DG_H8, KID_NORM_DG_W8, KID_NORM_DG_S16, KID_NORM_DG_M,
-    KID_NORM_BOTH_V8, KID_NORM_BOTH_H8, KID_NORM_BOTH_W8, KID_NORM_BOTH_S16, KID_NORM_BOTH_M,
+    KID_NORM_DX_V8, KID_NORM_DX_H8, KID_NORM_DX_W8, KID_NORM_DX_W16, KID_NORM_DX_S16, KID_NORM_DX_M,
+    KID_NORM_DG_V8, KID_NORM_DG_H8, KID_NORM_DG_W8, KID_NORM_DG_W16, KID_NORM_DG_S16, KID_NORM_DG_M,
+    KID_NORM_BOTH_V8, KID_NORM_BOTH_H8, KID_NORM_BOTH_W8, KID_NORM_BOTH_W16, KID_NORM_BOTH_S16, KID_NORM_BOTH_M,
     // attention with a bias of distances, launched kernels only: as above, and the bias's gradient (DB; DQB: with dq; with 128
     // channels one kernel for both spilled 119 registers: 2048 x 2048 of 16 heads, two images 850 us instead of 376 + 261)
     KID_ATTNB_W64, KID_ATTNB_W128, KID_ATTNB_DQ_W64, KID_ATTNB_DQ_W128, KID_ATTNB_DK_W64, KID_ATTNB_DK_W128, KID_ATTNB_DV_W64, KID_ATTNB_DV_W128,
@@ -80,7 +80,8 @@ constexpr bool is_attention_tile_kernel(int kid) { return (kid >= KID_ATTN_T64 &
 constexpr bool is_launched_attention_kernel(int kid) { return kid >= KID_ATTN_T64 && kid < KID_COUNT; }
 constexpr bool is_attention_kernel(int kid) { return kid >= KID_ROPE_4 && kid < KID_COUNT; }
 constexpr bool is_half_norm(int kid) { return kid == KID_NORM_H8 || kid == KID_NORM_H16 || kid == KID_NORM_DX_H8 || kid == KID_NORM_DG_H8 || kid == KID_NORM_BOTH_H8; }
-constexpr bool is_wide_norm(int kid) { return kid == KID_NORM_W16 || kid == KID_NORM_DX_W8 || kid == KID_NORM_DG_W8 || kid == KID_NORM_BOTH_W8; }
+constexpr bool is_norm_with_sums_in_lds(int kid) { return kid == KID_NORM_DG_W16 || kid == KID_NORM_BOTH_W16; }
+constexpr bool is_wide_norm(int kid) { return kid == KID_NORM_W16 || kid == KID_NORM_DX_W8 || kid == KID_NORM_DX_W16 || kid == KID_NORM_DG_W8 || kid == KID_NORM_BOTH_W8 || is_norm_with_sums_in_lds(kid); }
 constexpr bool is_train_kernel(int kid) { return kid >= KID_GEMM_PW_FWD && kid <= KID_SGD; }
 
 // the variant without / with a fused add_n of a kernel (ids without such a variant map to themselves / KID_NONE)

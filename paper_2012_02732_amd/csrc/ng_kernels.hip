@@ -105,7 +105,7 @@ constexpr int kSmemFloats = 5120;
 constexpr int kSmemFloatsPatch = 24 * 256, kSmemFloatsWide = 24 * 640;
 constexpr int attention_tile_floats(int kid), dbias_wave_floats();      // ng_attention_tiles.inc
 constexpr int smem_floats(int kid) {
-    return is_attention_tile_kernel(kid) ? attention_tile_floats(kid) : kid == KID_ATTNB_DB_W64 || kid == KID_ATTNB_DB_W128 ? dbias_wave_floats() : is_c3_patch(kid) ? 24 * c3_patches(kid) * c3_patch_pixels(kid) : kid == KID_PW_P32 ? 2 * kSmemFloatsPatch : is_pw_patch(kid) ? kSmemFloatsPatch : kSmemFloats;
+    return is_attention_tile_kernel(kid) ? attention_tile_floats(kid) : kid == KID_ATTNB_DB_W64 || kid == KID_ATTNB_DB_W128 ? dbias_wave_floats() : is_norm_with_sums_in_lds(kid) ? kSmemFloats + 2 * 16 * 1024 : is_c3_patch(kid) ? 24 * c3_patches(kid) * c3_patch_pixels(kid) : kid == KID_PW_P32 ? 2 * kSmemFloatsPatch : is_pw_patch(kid) ? kSmemFloatsPatch : kSmemFloats;
 }
 
 // ------------------------------------------------------------------------------------
@@ -2043,16 +2043,19 @@ NG_KERNEL(KID_NORM_DX_H8, NormArgs, "layer_norm_dgrad_half", norm_tile < NORM_DX
 NG_KERNEL(KID_NORM_DX_S16, NormArgs, "layer_norm_dgrad_few", norm_tile < NORM_DX, 256, 1, 16)
 NG_KERNEL(KID_NORM_DX_M, NormArgs, "layer_norm_dgrad_many", norm_many_tile < NORM_DX)
 NG_KERNEL(KID_NORM_DX_W8, NormArgs, "layer_norm_dgrad_wide", norm_tile < NORM_DX, 1024, 4, 8)
+NG_KERNEL(KID_NORM_DX_W16, NormArgs, "layer_norm_dgrad_wide_16", norm_tile < NORM_DX, 1024, 4, 16)
 NG_KERNEL(KID_NORM_DG_V8, NormArgs, "layer_norm_wgrad_8", norm_tile < NORM_DG, 256, 4, 8)
 NG_KERNEL(KID_NORM_DG_H8, NormArgs, "layer_norm_wgrad_half", norm_tile < NORM_DG, 512, 4, 8)
 NG_KERNEL(KID_NORM_DG_S16, NormArgs, "layer_norm_wgrad_few", norm_tile < NORM_DG, 256, 1, 16)
 NG_KERNEL(KID_NORM_DG_M, NormArgs, "layer_norm_wgrad_many", norm_many_tile < NORM_DG)
 NG_KERNEL(KID_NORM_DG_W8, NormArgs, "layer_norm_wgrad_wide", norm_tile < NORM_DG, 1024, 4, 8)
+NG_KERNEL(KID_NORM_DG_W16, NormArgs, "layer_norm_wgrad_wide_16", norm_tile < NORM_DG, 1024, 4, 16)
 NG_KERNEL(KID_NORM_BOTH_V8, NormArgs, "layer_norm_dgrad+wgrad_8", norm_tile < NORM_BOTH, 256, 4, 8)
 NG_KERNEL(KID_NORM_BOTH_H8, NormArgs, "layer_norm_dgrad+wgrad_half", norm_tile < NORM_BOTH, 512, 4, 8)
 NG_KERNEL(KID_NORM_BOTH_S16, NormArgs, "layer_norm_dgrad+wgrad_few", norm_tile < NORM_BOTH, 256, 1, 16)
 NG_KERNEL(KID_NORM_BOTH_M, NormArgs, "layer_norm_dgrad+wgrad_many", norm_many_tile < NORM_BOTH)
 NG_KERNEL(KID_NORM_BOTH_W8, NormArgs, "layer_norm_dgrad+wgrad_wide", norm_tile < NORM_BOTH, 1024, 4, 8)
+NG_KERNEL(KID_NORM_BOTH_W16, NormArgs, "layer_norm_dgrad+wgrad_wide_16", norm_tile < NORM_BOTH, 1024, 4, 16)
 NG_KERNEL(KID_ATTNB_W64, AttnArgs, "attention_biased_wave_64", attention_wave_tile < 4, true)
 NG_KERNEL(KID_ATTNB_W128, AttnArgs, "attention_biased_wave_128", attention_wave_tile < 8, true)
 NG_KERNEL(KID_ATTNB_DQ_W64, AttnArgs, "attention_biased_dq_wave_64", attention_dq_wave_tile < 4, true)
@@ -2106,9 +2109,9 @@ NG_KERNEL0(KID_SGD_BATCH, SgdBatchArgs, "sgd_update_batch", sgd_batch_tile)
     X(KID_ATTN_DK_T64) X(KID_ATTN_DK_T128) X(KID_ATTN_DV_T64) X(KID_ATTN_DV_T128)    \
     X(KID_ATTN_DKV_T64) X(KID_ROPE_BOTH_4) X(KID_ROPE_BOTH_8) X(KID_ROPE_BOTH_N)    \
     X(KID_NORM_V8) X(KID_NORM_V16) X(KID_NORM_S16) X(KID_NORM_M) X(KID_NORM_H8) X(KID_NORM_H16) X(KID_NORM_W16)    \
-    X(KID_NORM_DX_V8) X(KID_NORM_DX_H8) X(KID_NORM_DX_S16) X(KID_NORM_DX_M) X(KID_NORM_DX_W8)    \
-    X(KID_NORM_DG_V8) X(KID_NORM_DG_H8) X(KID_NORM_DG_S16) X(KID_NORM_DG_M) X(KID_NORM_DG_W8)    \
-    X(KID_NORM_BOTH_V8) X(KID_NORM_BOTH_H8) X(KID_NORM_BOTH_S16) X(KID_NORM_BOTH_M) X(KID_NORM_BOTH_W8)    \
+    X(KID_NORM_DX_V8) X(KID_NORM_DX_H8) X(KID_NORM_DX_S16) X(KID_NORM_DX_M) X(KID_NORM_DX_W8) X(KID_NORM_DX_W16)    \
+    X(KID_NORM_DG_V8) X(KID_NORM_DG_H8) X(KID_NORM_DG_S16) X(KID_NORM_DG_M) X(KID_NORM_DG_W8) X(KID_NORM_DG_W16)    \
+    X(KID_NORM_BOTH_V8) X(KID_NORM_BOTH_H8) X(KID_NORM_BOTH_S16) X(KID_NORM_BOTH_M) X(KID_NORM_BOTH_W8) X(KID_NORM_BOTH_W16)    \
     X(KID_DROPOUT) X(KID_POSITION_BIAS) X(KID_POSITION_BIAS_WGRAD)    \
     X(KID_ATTNB_W64) X(KID_ATTNB_W128) X(KID_ATTNB_DQ_W64) X(KID_ATTNB_DQ_W128) X(KID_ATTNB_DK_W64) X(KID_ATTNB_DK_W128)    \
     X(KID_ATTNB_DV_W64) X(KID_ATTNB_DV_W128) X(KID_ATTNB_T64) X(KID_ATTNB_T128) X(KID_ATTNB_DQ_T64) X(KID_ATTNB_DQ_T128)    \

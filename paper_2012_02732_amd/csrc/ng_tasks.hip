@@ -238,6 +238,7 @@ static int pair_kid(const Task& first, const Task& second) {
     if (kid_first == KID_NORM_DX_S16 && kid_second == KID_NORM_DG_S16) return KID_NORM_BOTH_S16;
     if (kid_first == KID_NORM_DX_M && kid_second == KID_NORM_DG_M) return KID_NORM_BOTH_M;
     if (kid_first == KID_NORM_DX_W8 && kid_second == KID_NORM_DG_W8) return KID_NORM_BOTH_W8;
+    if (kid_first == KID_NORM_DX_W16 && kid_second == KID_NORM_DG_W16) return KID_NORM_BOTH_W16;
     return KID_NONE;
 }
 bool can_pair(const Task& first, const Task& second) {
@@ -328,6 +329,7 @@ void make_pair_task(const Task& first, const Task& second, Task& t) {
         case KID_NORM_BOTH_S16: set_norm_backward<KID_NORM_BOTH_S16>(first, second, t); break;
         case KID_NORM_BOTH_M: set_norm_backward<KID_NORM_BOTH_M>(first, second, t); break;
         case KID_NORM_BOTH_W8: set_norm_backward<KID_NORM_BOTH_W8>(first, second, t); break;
+        case KID_NORM_BOTH_W16: set_norm_backward<KID_NORM_BOTH_W16>(first, second, t); break;
         default: t = first; break;
     }
 }
@@ -832,16 +834,17 @@ NormPlan norm_plan(const ng_graph* g, int v) {
         // images of 1000 channels, 300 tokens in 160 of 1024 threads 29.3, in twice as many of 512 26.2), since what a workgroup reads of a channel
         // should be whole lines of memory. TB/s of the forward kernel with 2 / 4 / 8 of them, 16 images of 512 channels, 8192 tokens 3.3 / 4.1 / 5.1, of
         // 1024 channels, 4096 tokens 2.9 / 3.9 / 4.8; both gradients in one launch 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9. Eight take 512 threads for more than 256
-        // channels, 1024 for more than 512 (forward: 1024), in fewer and larger workgroups: not faster where the tensors come out of the 256 MB cache
+        // channels, 1024 for more than 512 (forward: 1024), or 16 channels a thread, in fewer and larger workgroups: not faster where the tensors come out of the 256 MB cache
         // behind the L2s (4 images of 2048 channels, 4096 tokens 4: 44 us, 8: 51), so only for larger ones (both gradients of 8
         // images of 1024 channels, 4096 tokens, 400 MB, 4: 121, 8: 115; of 2048 tokens 49 and 58). A forward kernel of 512 threads with 16 channels each takes the place of 1024 with 8: 123 -> 113 us and, in
-        // the cache, 53 -> 39 (16 and 8 images of 1024 channels, 4096 tokens, 8 side by side).
+        // the cache, 53 -> 39 (16 and 8 images of 1024 channels, 4096 tokens, 8 side by side). Gradients of 16 channels a thread read dy twice, but twice as
+        // many tokens side by side: both of 2 images of 4096 channels, 8192 / 2000 tokens 2: 397 / 71, 4: 313 / 67 us, of 8 of 2048, 4096 tokens 4: 262, 8: 225.
         const bool large = (double)x.elems() * 4 * (which == 0 ? 2 : 3) > 268435456.0;
         long threads = 0;
         for (int log2 = 3; log2 >= 0; --log2) {
             const long lanes = 1L << log2;
             threads = ceil_div(C * lanes, 8);
-            if (log2 > 0 && (2 * lanes >= T || threads > (which == 0 ? 2048 : 1024) || x.n * ceil_div(T, 4 * lanes) < (threads <= kBlock ? 64 : threads <= 512 ? 128 : 256))) continue;
+            if (log2 > 0 && (2 * lanes >= T || threads > 2048 || x.n * ceil_div(T, 4 * lanes) < (threads <= kBlock ? 64 : threads <= 512 ? 128 : 256))) continue;
             if (log2 == 3 && threads > kBlock && !large) continue;
             p.lanes_log2 = log2;
             break;
@@ -849,7 +852,7 @@ NormPlan norm_plan(const ng_graph* g, int v) {
         p.kid = threads <= kBlock ? one_of(KID_NORM_V8, KID_NORM_DX_V8, KID_NORM_DG_V8)
               : which == 0 && p.lanes_log2 == 0 ? (int)KID_NORM_V16            // few tokens: a kernel that the device-resident replay has as well
               : threads <= 512 ? one_of(KID_NORM_H8, KID_NORM_DX_H8, KID_NORM_DG_H8)
-              : threads <= 1024 ? one_of(KID_NORM_H16, KID_NORM_DX_W8, KID_NORM_DG_W8) : (int)KID_NORM_W16;      // (16 channels a thread)
+              : threads <= 1024 ? one_of(KID_NORM_H16, KID_NORM_DX_W8, KID_NORM_DG_W8) : one_of(KID_NORM_W16, KID_NORM_DX_W16, KID_NORM_DG_W16);      // (16 channels a thread)
         p.blocks = (int)ceil_div(T, 4L << p.lanes_log2);
         if (p.kid != KID_NORM_DG_V8) most = 256;                // one workgroup of so many threads and registers on a compute unit, all of them at once
     }
