@@ -820,7 +820,9 @@ NormPlan norm_plan(const ng_graph* g, int v) {
     const bool wgrad = nd.op == NG_OP_LAYER_NORM_WGRAD;
     long most = 512;                                           // workgroups of wgrad
     auto one_of = [which](int forward, int dgrad, int wgrad) { return which == 0 ? forward : which == 1 ? dgrad : wgrad; };
-    if (C > 4096 || (T < 4 && C * T > 4096)) {
+    // (What no workgroup holds in registers is read again for each sum, much slower: 2 images of 5120 channels, 2048 tokens, with gradients, in 1024
+    // threads of 16 channels each 202 us, read again 972; 8192 channels, 8192 tokens 666 and 2079.)
+    if (C > 16384 || (T < 4 && C * T > 4096)) {
         p.kid = one_of(KID_NORM_M, KID_NORM_DX_M, KID_NORM_DG_M);
         while (p.lanes_log2 < 4 && (1L << p.lanes_log2) < T) ++p.lanes_log2;
         p.blocks = (int)ceil_div(T, 1L << p.lanes_log2);
@@ -850,7 +852,7 @@ NormPlan norm_plan(const ng_graph* g, int v) {
             break;
         }
         p.kid = threads <= kBlock ? one_of(KID_NORM_V8, KID_NORM_DX_V8, KID_NORM_DG_V8)
-              : which == 0 && p.lanes_log2 == 0 ? (int)KID_NORM_V16            // few tokens: a kernel that the device-resident replay has as well
+              : which == 0 && p.lanes_log2 == 0 && threads <= 512 ? (int)KID_NORM_V16            // few tokens: a kernel that the device-resident replay has as well
               : threads <= 512 ? one_of(KID_NORM_H8, KID_NORM_DX_H8, KID_NORM_DG_H8)
               : threads <= 1024 ? one_of(KID_NORM_H16, KID_NORM_DX_W8, KID_NORM_DG_W8) : one_of(KID_NORM_W16, KID_NORM_DX_W16, KID_NORM_DG_W16);      // (16 channels a thread)
         p.blocks = (int)ceil_div(T, 4L << p.lanes_log2);

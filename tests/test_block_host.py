@@ -112,7 +112,7 @@ def test_work_of_the_block_operators():
 
 NORM_KERNELS = [                # n, c, h, w, name of the forward kernel, what the gradients' end in
     (8, 1024, 1, 1, "layer_norm_few", "few"), (2, 7, 1, 3, "layer_norm_few", "few"), (1, 2000, 1, 3, "layer_norm_many", "many"), (1, 4097, 1, 1, "layer_norm_many", "many"),
-    (2, 5000, 1, 18, "layer_norm_many", "many"), (6, 520, 1, 333, "layer_norm_8", "8"), (2, 33, 3, 7, "layer_norm_8", "8"), (1, 2048, 2, 8, "layer_norm_8", "8"),
+    (2, 5000, 1, 18, "layer_norm_half_16", "wide"), (1, 16385, 1, 18, "layer_norm_many", "many"), (1, 16384, 1, 21, "layer_norm_wide_16", "wide_16"), (1, 4097, 1, 9, "layer_norm_half_16", "wide"), (6, 520, 1, 333, "layer_norm_8", "8"), (2, 33, 3, 7, "layer_norm_8", "8"), (1, 2048, 2, 8, "layer_norm_8", "8"),
     (1, 4096, 1, 4, "layer_norm_16", "half"), (16, 600, 1, 259, "layer_norm_half", "half"), (16, 1100, 1, 300, "layer_norm_half_16", "wide"), (16, 2100, 1, 259, "layer_norm_wide_16", "wide_16"),
     (2, 4096, 1, 8192, "layer_norm_wide_16", "wide_16"), (8, 1024, 1, 4096, "layer_norm_half", "wide"), (16, 1024, 1, 4096, "layer_norm_half_16", "wide"), (16, 512, 1, 8192, "layer_norm_half", "half"),
 ]

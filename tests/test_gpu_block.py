@@ -24,6 +24,7 @@ NORM = [                        # n, c, h, w
     (1, 1, 1, 1), (1, 1, 2, 9), (2, 3, 1, 2), (3, 5, 1, 3), (2, 7, 1, 5), (1, 64, 1, 4), (8, 1024, 1, 1), (5, 1023, 1, 1), (2, 1300, 1, 2), (2, 257, 3, 7), (1, 600, 1, 17), (4, 96, 1, 31),
     (2, 1025, 1, 33), (1, 2048, 2, 8), (1, 4096, 1, 9), (3, 2047, 1, 3), (1, 4097, 1, 3), (2, 5000, 1, 18), (1, 9001, 1, 1), (16, 1100, 1, 259), (130, 4, 1, 37), (700, 40, 1, 6),
     (513, 33, 1, 1), (6, 520, 1, 333), (16, 600, 1, 259), (17, 2100, 1, 255), (40, 700, 1, 300), (3, 3000, 1, 350), (33, 200, 1, 260), (2, 1, 1, 9001),
+    (1, 16500, 1, 18), (1, 16384, 1, 21), (3, 12001, 1, 9), (2, 8200, 1, 530), (2, 5121, 1, 2051),
 ]
 
 
