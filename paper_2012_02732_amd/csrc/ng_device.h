@@ -474,6 +474,12 @@ struct NormArgs {
     int items, per_tile;       // blocks of all images, and how many of them a workgroup walks
     int tiles;
 };
+// Where a layer norm's workgroup has its channels in an image [C][T], as byte offsets: thread `row` has the channels row, row + rows, .., the k-th
+// of them at what is its own (norm_lane, of its first channel and token `t0`) plus what all share (norm_turn). A channel or token that does
+// not exist is outside by the thread's own, kOutside, and the shared one is below 2^31 - 0 where no thread has a channel: a workgroup's
+// registers hold more channels than a small C has, k rows T bytes times four may be anything - so that the sum is never inside again.
+constexpr unsigned norm_lane(bool on, int row, int T, int t0) { return on ? 4u * ((unsigned)row * (unsigned)T + (unsigned)t0) : kOutside; }
+constexpr unsigned norm_turn(int k, int rows, int C, int T) { return k * rows < C ? 4u * (unsigned)(k * rows) * (unsigned)T : 0u; }
 struct DropoutArgs {
     const float* x;
     const float* seed;         // two words

@@ -1,0 +1,60 @@
+"""Layer norm without a GPU: where its kernels read and write."""
+import os
+import re
+import subprocess
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2012_02732_amd", "csrc")
+
+
+def test_offsets_of_a_norm_stay_in_their_image(tmp_path):
+    """Every channel that exists is where it belongs, and what does not exist, channel or token, is outside for a load, which is checked by the
+    thread's own part alone, and for a store, whose parts are added up in 32 bits: for workgroups of every size and form over images of up to
+    2^29 values, few channels of millions of tokens among them (8 of 4096 x 4096: a turn of the channels is 2^31 bytes)."""
+    src = tmp_path / "offsets.cpp"
+    src.write_text(r"""
+#include <cstdio>
+#include <initializer_list>
+#include "ng_device.h"
+using u64 = unsigned long long;
+static int check(int threads, int K, int lanes, u64 C, u64 T) {
+    const int rows = threads / lanes;
+    const u64 bytes = 4 * C * T;
+    for (int k = 0; k < K; ++k) {
+        const u64 shared = ng::norm_turn(k, rows, (int)C, (int)T);
+        if (shared >= (1ull << 31)) return 1;
+        for (int row = 0; row < rows; ++row) {
+            const u64 c = row + (u64)k * rows;
+            for (u64 t : {(u64)0, T / 2, T - 1}) {
+                const unsigned own = ng::norm_lane(c < C, row, (int)T, (int)t), sum = own + (unsigned)shared;
+                if (c < C ? !(own < bytes && sum == 4 * (c * T + t) && (u64)own + shared < bytes) : !(own >= bytes && sum >= bytes)) return 2;
+            }
+            const unsigned none = ng::norm_lane(false, row, (int)T, 0);
+            if (none < bytes || none + (unsigned)shared < bytes) return 3;
+        }
+    }
+    return 0;
+}
+int main() {
+    const u64 most = 1ull << 29;
+    for (int threads : {256, 512, 1024})
+        for (int K : {8, 16})
+            for (int lanes : {1, 2, 4, 8})
+                for (u64 C : {1, 2, 3, 7, 8, 31, 32, 33, 64, 127, 128, 129, 520, 1000, 1023, 1024, 2047, 4096, 8192, 16384}) {
+                    if (C > (u64)K * threads / lanes) continue;
+                    for (u64 T : {(u64)1, (u64)3, (u64)4, (u64)333, (u64)65536, (u64)1000000, (u64)1 << 22, (u64)2500000, (u64)1 << 24, most / C - 1, most / C})
+                        if (T > 0 && C * T <= most)
+                            if (const int what = check(threads, K, lanes, C, T)) return std::printf("%d: %d threads of %d channels, %d side by side, %llu x %llu\n", what, threads, K, lanes, C, T), 1;
+                }
+    std::puts("ok");
+}
+""")
+    exe = str(tmp_path / "offsets")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "include"), "-I", CSRC, str(src), "-o", exe], check=True)
+    done = subprocess.run([exe], capture_output=True, text=True)
+    assert (done.returncode, done.stdout.strip()) == (0, "ok")
+    # and the kernels take their offsets from nowhere else
+    kernels = open(os.path.join(CSRC, "ng_block_tiles.inc")).read()
+    calls = re.findall(r"norm_(?:load|store)<V(?:, FIN)?>\(\w+, (.*)\);", kernels)
+    assert len(calls) == 7 and all("turn(" in call and re.match(r"(on \? |\w*row \+ k \* rows < a\.C \? )?(lane_at|store_at|at)( : kOutside)?, ", call) for call in calls), calls
+    assert kernels.count("lane_at = norm_lane(") == 1 and len(re.findall(r"= norm_turn\(|return norm_turn\(", kernels)) == 1
