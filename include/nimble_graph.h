@@ -122,7 +122,7 @@ enum {
     /* Around the attention of a transformer block. */
     NG_OP_LAYER_NORM = 33,    /* preds {x}, weights {gamma[c], beta[c]}: over the c channels of each pixel (token), y = gamma (x - mean) /
                                  sqrt(variance + eps) + beta, variance the mean of (x - mean)^2. c h w <= 2^29. (Up to 16384 channels
-                                 - of fewer than four pixels 4096 - are read once, more of them once for each sum.) */
+                                 - of one pixel 4096, of two 2048, of three 1024 - are read once, more of them once for each sum.) */
     NG_OP_LAYER_NORM_DGRAD = 34, /* preds {dy, x}, same weights, eps -> dx */
     NG_OP_LAYER_NORM_WGRAD = 35, /* preds {dy, x}, same weights, eps -> [2][c][1][1]: dgamma, then dbeta */
     NG_OP_DROPOUT = 36,       /* preds {x, seed} or {x, seed, residual}: y = (residual +) (kept ? x / (1 - rate) : 0), x and residual of one

@@ -161,6 +161,14 @@ constexpr bool in_build(int build, int kid) {
 
 constexpr int kBlock = 256;          // threads that work on one tile (a stand-alone kernel's workgroup)
 constexpr int block_threads(int kid) { return is_wide_norm(kid) ? 1024 : is_half_norm(kid) ? 512 : kBlock; }      // (kernels that are only launched may have more)
+// Channels that a thread of a layer norm's kernel has in registers, 0: none is kept, any number; and those that its workgroup has, with
+// 2^lanes_log2 threads side by side along the tokens.
+constexpr int norm_turns(int kid) {
+    return kid == KID_NORM_M || kid == KID_NORM_DX_M || kid == KID_NORM_DG_M || kid == KID_NORM_BOTH_M ? 0
+         : kid == KID_NORM_V16 || kid == KID_NORM_H16 || kid == KID_NORM_W16 || kid == KID_NORM_DX_W16 || is_norm_with_sums_in_lds(kid) || kid == KID_NORM_S16 ||
+           kid == KID_NORM_DX_S16 || kid == KID_NORM_DG_S16 || kid == KID_NORM_BOTH_S16 ? 16 : 8;
+}
+constexpr long norm_channels(int kid, int lanes_log2) { return norm_turns(kid) == 0 ? 1L << 31 : (long)norm_turns(kid) * (block_threads(kid) >> lanes_log2); }
 constexpr int kSubs = 2;             // tiles a workgroup of the resident kernel works on at a time
 constexpr int kGroup = kBlock * kSubs;  // threads per workgroup of the resident kernel
 constexpr int kArgBytes = 256;       // size of the per-task argument block of the resident kernel's task table

@@ -2031,31 +2031,33 @@ NG_KERNEL(KID_ATTN_DKV_T64, PairAttnArgs, "attention_dk+dv_tile_64", attention_d
 NG_KERNEL(KID_ROPE_BOTH_4, RopeArgs, "head_rope_dgrad+wgrad_128", rope_tile < ROPE_BOTH, 4)
 NG_KERNEL(KID_ROPE_BOTH_8, RopeArgs, "head_rope_dgrad+wgrad_256", rope_tile < ROPE_BOTH, 8)
 NG_KERNEL(KID_ROPE_BOTH_N, RopeArgs, "head_rope_dgrad+wgrad_few", rope_few_tile < ROPE_BOTH)
-NG_KERNEL(KID_NORM_V8, NormArgs, "layer_norm_8", norm_tile < NORM_FWD, 256, 4, 8)
-NG_KERNEL(KID_NORM_V16, NormArgs, "layer_norm_16", norm_tile < NORM_FWD, 256, 4, 16)
-NG_KERNEL(KID_NORM_S16, NormArgs, "layer_norm_few", norm_tile < NORM_FWD, 256, 1, 16)
+#define NG_NORM(KID, NAME, MODE, V) NG_KERNEL(KID, NormArgs, NAME, norm_tile < MODE, block_threads(KID), V, norm_turns(KID))
+NG_NORM(KID_NORM_V8, "layer_norm_8", NORM_FWD, 4)
+NG_NORM(KID_NORM_V16, "layer_norm_16", NORM_FWD, 4)
+NG_NORM(KID_NORM_S16, "layer_norm_few", NORM_FWD, 1)
 NG_KERNEL(KID_NORM_M, NormArgs, "layer_norm_many", norm_many_tile < NORM_FWD)
-NG_KERNEL(KID_NORM_H8, NormArgs, "layer_norm_half", norm_tile < NORM_FWD, 512, 4, 8)
-NG_KERNEL(KID_NORM_H16, NormArgs, "layer_norm_half_16", norm_tile < NORM_FWD, 512, 4, 16)
-NG_KERNEL(KID_NORM_W16, NormArgs, "layer_norm_wide_16", norm_tile < NORM_FWD, 1024, 4, 16)
-NG_KERNEL(KID_NORM_DX_V8, NormArgs, "layer_norm_dgrad_8", norm_tile < NORM_DX, 256, 4, 8)
-NG_KERNEL(KID_NORM_DX_H8, NormArgs, "layer_norm_dgrad_half", norm_tile < NORM_DX, 512, 4, 8)
-NG_KERNEL(KID_NORM_DX_S16, NormArgs, "layer_norm_dgrad_few", norm_tile < NORM_DX, 256, 1, 16)
+NG_NORM(KID_NORM_H8, "layer_norm_half", NORM_FWD, 4)
+NG_NORM(KID_NORM_H16, "layer_norm_half_16", NORM_FWD, 4)
+NG_NORM(KID_NORM_W16, "layer_norm_wide_16", NORM_FWD, 4)
+NG_NORM(KID_NORM_DX_V8, "layer_norm_dgrad_8", NORM_DX, 4)
+NG_NORM(KID_NORM_DX_H8, "layer_norm_dgrad_half", NORM_DX, 4)
+NG_NORM(KID_NORM_DX_S16, "layer_norm_dgrad_few", NORM_DX, 1)
 NG_KERNEL(KID_NORM_DX_M, NormArgs, "layer_norm_dgrad_many", norm_many_tile < NORM_DX)
-NG_KERNEL(KID_NORM_DX_W8, NormArgs, "layer_norm_dgrad_wide", norm_tile < NORM_DX, 1024, 4, 8)
-NG_KERNEL(KID_NORM_DX_W16, NormArgs, "layer_norm_dgrad_wide_16", norm_tile < NORM_DX, 1024, 4, 16)
-NG_KERNEL(KID_NORM_DG_V8, NormArgs, "layer_norm_wgrad_8", norm_tile < NORM_DG, 256, 4, 8)
-NG_KERNEL(KID_NORM_DG_H8, NormArgs, "layer_norm_wgrad_half", norm_tile < NORM_DG, 512, 4, 8)
-NG_KERNEL(KID_NORM_DG_S16, NormArgs, "layer_norm_wgrad_few", norm_tile < NORM_DG, 256, 1, 16)
+NG_NORM(KID_NORM_DX_W8, "layer_norm_dgrad_wide", NORM_DX, 4)
+NG_NORM(KID_NORM_DX_W16, "layer_norm_dgrad_wide_16", NORM_DX, 4)
+NG_NORM(KID_NORM_DG_V8, "layer_norm_wgrad_8", NORM_DG, 4)
+NG_NORM(KID_NORM_DG_H8, "layer_norm_wgrad_half", NORM_DG, 4)
+NG_NORM(KID_NORM_DG_S16, "layer_norm_wgrad_few", NORM_DG, 1)
 NG_KERNEL(KID_NORM_DG_M, NormArgs, "layer_norm_wgrad_many", norm_many_tile < NORM_DG)
-NG_KERNEL(KID_NORM_DG_W8, NormArgs, "layer_norm_wgrad_wide", norm_tile < NORM_DG, 1024, 4, 8)
-NG_KERNEL(KID_NORM_DG_W16, NormArgs, "layer_norm_wgrad_wide_16", norm_tile < NORM_DG, 1024, 4, 16)
-NG_KERNEL(KID_NORM_BOTH_V8, NormArgs, "layer_norm_dgrad+wgrad_8", norm_tile < NORM_BOTH, 256, 4, 8)
-NG_KERNEL(KID_NORM_BOTH_H8, NormArgs, "layer_norm_dgrad+wgrad_half", norm_tile < NORM_BOTH, 512, 4, 8)
-NG_KERNEL(KID_NORM_BOTH_S16, NormArgs, "layer_norm_dgrad+wgrad_few", norm_tile < NORM_BOTH, 256, 1, 16)
+NG_NORM(KID_NORM_DG_W8, "layer_norm_wgrad_wide", NORM_DG, 4)
+NG_NORM(KID_NORM_DG_W16, "layer_norm_wgrad_wide_16", NORM_DG, 4)
+NG_NORM(KID_NORM_BOTH_V8, "layer_norm_dgrad+wgrad_8", NORM_BOTH, 4)
+NG_NORM(KID_NORM_BOTH_H8, "layer_norm_dgrad+wgrad_half", NORM_BOTH, 4)
+NG_NORM(KID_NORM_BOTH_S16, "layer_norm_dgrad+wgrad_few", NORM_BOTH, 1)
 NG_KERNEL(KID_NORM_BOTH_M, NormArgs, "layer_norm_dgrad+wgrad_many", norm_many_tile < NORM_BOTH)
-NG_KERNEL(KID_NORM_BOTH_W8, NormArgs, "layer_norm_dgrad+wgrad_wide", norm_tile < NORM_BOTH, 1024, 4, 8)
-NG_KERNEL(KID_NORM_BOTH_W16, NormArgs, "layer_norm_dgrad+wgrad_wide_16", norm_tile < NORM_BOTH, 1024, 4, 16)
+NG_NORM(KID_NORM_BOTH_W8, "layer_norm_dgrad+wgrad_wide", NORM_BOTH, 4)
+NG_NORM(KID_NORM_BOTH_W16, "layer_norm_dgrad+wgrad_wide_16", NORM_BOTH, 4)
+#undef NG_NORM
 NG_KERNEL(KID_ATTNB_W64, AttnArgs, "attention_biased_wave_64", attention_wave_tile < 4, true)
 NG_KERNEL(KID_ATTNB_W128, AttnArgs, "attention_biased_wave_128", attention_wave_tile < 8, true)
 NG_KERNEL(KID_ATTNB_DQ_W64, AttnArgs, "attention_biased_dq_wave_64", attention_dq_wave_tile < 4, true)

@@ -820,15 +820,16 @@ NormPlan norm_plan(const ng_graph* g, int v) {
     const bool wgrad = nd.op == NG_OP_LAYER_NORM_WGRAD;
     long most = 512;                                           // workgroups of wgrad
     auto one_of = [which](int forward, int dgrad, int wgrad) { return which == 0 ? forward : which == 1 ? dgrad : wgrad; };
+    if (T < 4)
+        while ((1L << p.lanes_log2) < T) ++p.lanes_log2;
     // (What no workgroup holds in registers is read again for each sum, much slower: 2 images of 5120 channels, 2048 tokens, with gradients, in 1024
     // threads of 16 channels each 202 us, read again 972; 8192 channels, 8192 tokens 666 and 2079.)
-    if (C > 16384 || (T < 4 && C * T > 4096)) {
+    if (C > norm_channels(T < 4 ? KID_NORM_S16 : KID_NORM_W16, T < 4 ? p.lanes_log2 : 0)) {
         p.kid = one_of(KID_NORM_M, KID_NORM_DX_M, KID_NORM_DG_M);
         while (p.lanes_log2 < 4 && (1L << p.lanes_log2) < T) ++p.lanes_log2;
         p.blocks = (int)ceil_div(T, 1L << p.lanes_log2);
     } else if (T < 4) {
         p.kid = one_of(KID_NORM_S16, KID_NORM_DX_S16, KID_NORM_DG_S16);
-        p.lanes_log2 = T == 1 ? 0 : T == 2 ? 1 : 2;
     } else {
         // Threads side by side along the tokens: as many as leave 64 workgroups, 128 of more than 256 threads, 256 of more than 512 (few workgroups have few
         // rows of sums to join: forward and both gradients of 4 images of 256 channels, 400 tokens with at least 64 / 128 / 256 workgroups 15.4 /
@@ -1528,6 +1529,7 @@ int build_task(ng_graph* g, int v, char* arena, float* packed, Task& t) {
             }
             a.eps = nd.p.eps, a.C = (int)x.c, a.T = (int)(x.h * x.w);
             a.lanes_log2 = p.lanes_log2, a.blocks = p.blocks, a.items = p.items, a.per_tile = p.per_tile, a.tiles = (int)p.tiles;
+            if (norm_channels(p.kid, p.lanes_log2) < x.c) return g->fail(NG_EINVAL, "node %d: the norm's kernel does not hold %lld channels", v, (long long)x.c);
             set_any_kernel(t, p.kid, a, p.tiles);
             break;
         }

@@ -1,7 +1,12 @@
-"""Layer norm without a GPU: where its kernels read and write."""
+"""Layer norm without a GPU: where its kernels read and write, and what they hold."""
 import os
 import re
 import subprocess
+
+import numpy as np
+import pytest
+
+from block_util import kernels, norm_graph
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2012_02732_amd", "csrc")
@@ -58,3 +63,26 @@ int main() {
     calls = re.findall(r"norm_(?:load|store)<V(?:, FIN)?>\(\w+, (.*)\);", kernels)
     assert len(calls) == 7 and all("turn(" in call and re.match(r"(on \? |\w*row \+ k \* rows < a\.C \? )?(lane_at|store_at|at)( : kOutside)?, ", call) for call in calls), calls
     assert kernels.count("lane_at = norm_lane(") == 1 and len(re.findall(r"= norm_turn\(|return norm_turn\(", kernels)) == 1
+
+
+HELD = {"8": (256, 8), "16": (256, 16), "few": (256, 16), "half": (512, 8), "half_16": (512, 16), "wide": (1024, 8), "wide_16": (1024, 16)}      # threads, channels of each
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5, 9, 33, 260, 5000])
+def test_the_kernel_of_a_norm_holds_its_channels(tokens):
+    """What a workgroup has in registers is at least all channels of its tokens: with one to three tokens, 1, 2 and 4 threads side by side (three
+    tokens of 1025 to 1365 channels are 3075 to 4095 values, but 1024 channels are all that 64 threads have)."""
+    side_by_side = {1: 1, 2: 2, 3: 4}.get(tokens, 1)
+    for n in (1, 16):
+        for c in (1, 8, 255, 520, 1023, 1024, 1025, 1100, 1365, 1366, 2047, 2048, 2049, 4095, 4096, 4097, 8192, 8193, 16384, 16385):
+            g = norm_graph(*(np.zeros(s, np.float32) for s in ((1, 1, 1, 1), 1, 1, (1, 1, 1, 1))), 1e-5)
+            for name in ("x", "dy"):                            # the shapes alone
+                g.nodes[g.names[name]].params = dict(n=n, c=c, h=1, w=tokens)
+            for name, kernel in kernels(g).items():
+                how = re.fullmatch("layer_norm_(?:dgrad_|wgrad_)?(.*)", kernel).group(1)
+                most = 16 * (256 // side_by_side) if tokens < 4 else 16384
+                if how == "many":                               # read again for each sum: any number
+                    assert c > most, (n, c, tokens, kernel)
+                else:
+                    threads, turns = HELD[how]
+                    assert c <= min(most, turns * (threads // side_by_side)), (n, c, tokens, kernel)
