@@ -483,11 +483,12 @@ struct NormArgs {
     int tiles;
 };
 // Where a layer norm's workgroup has its channels in an image [C][T], as byte offsets: thread `row` has the channels row, row + rows, .., the k-th
-// of them at what is its own (norm_lane, of its first channel and token `t0`) plus what all share (norm_turn). A channel or token that does
-// not exist is outside by the thread's own, kOutside, and the shared one is below 2^31 - 0 where no thread has a channel: a workgroup's
-// registers hold more channels than a small C has, k rows T bytes times four may be anything - so that the sum is never inside again.
+// of them at what is its own (norm_lane, of its first channel and token `t0`; kOutside for a channel or token that does not exist) plus k
+// turns, which all share. A workgroup's registers hold more channels than a small C has, so for what does not exist k turns may be anything.
+// Loads pass the two apart, and the thread's own is checked; a store's are added up, and not past 2^32, which would be inside again.
 constexpr unsigned norm_lane(bool on, int row, int T, int t0) { return on ? 4u * ((unsigned)row * (unsigned)T + (unsigned)t0) : kOutside; }
-constexpr unsigned norm_turn(int k, int rows, int C, int T) { return k * rows < C ? 4u * (unsigned)(k * rows) * (unsigned)T : 0u; }
+constexpr unsigned norm_turn(int rows, int T) { return 4u * (unsigned)rows * (unsigned)T; }
+constexpr unsigned norm_store_at(unsigned lane, unsigned shared) { return lane + shared < lane ? ~0u : lane + shared; }      // (one instruction)
 struct DropoutArgs {
     const float* x;
     const float* seed;         // two words

@@ -26,16 +26,15 @@ static int check(int threads, int K, int lanes, u64 C, u64 T) {
     const int rows = threads / lanes;
     const u64 bytes = 4 * C * T;
     for (int k = 0; k < K; ++k) {
-        const u64 shared = ng::norm_turn(k, rows, (int)C, (int)T);
-        if (shared >= (1ull << 31)) return 1;
+        const unsigned shared = (unsigned)k * ng::norm_turn(rows, (int)T);
         for (int row = 0; row < rows; ++row) {
             const u64 c = row + (u64)k * rows;
             for (u64 t : {(u64)0, T / 2, T - 1}) {
-                const unsigned own = ng::norm_lane(c < C, row, (int)T, (int)t), sum = own + (unsigned)shared;
-                if (c < C ? !(own < bytes && sum == 4 * (c * T + t) && (u64)own + shared < bytes) : !(own >= bytes && sum >= bytes)) return 2;
+                const unsigned own = ng::norm_lane(c < C, row, (int)T, (int)t), sum = ng::norm_store_at(own, shared);
+                if (c < C ? !(own < bytes && sum == 4 * (c * T + t) && (u64)own + shared < bytes) : !(own >= bytes && sum >= bytes)) return 1;
             }
             const unsigned none = ng::norm_lane(false, row, (int)T, 0);
-            if (none < bytes || none + (unsigned)shared < bytes) return 3;
+            if (none < bytes || ng::norm_store_at(none, shared) < bytes) return 2;
         }
     }
     return 0;
@@ -61,8 +60,9 @@ int main() {
     # and the kernels take their offsets from nowhere else
     kernels = open(os.path.join(CSRC, "ng_block_tiles.inc")).read()
     calls = re.findall(r"norm_(?:load|store)<V(?:, FIN)?>\(\w+, (.*)\);", kernels)
-    assert len(calls) == 7 and all("turn(" in call and re.match(r"(on \? |\w*row \+ k \* rows < a\.C \? )?(lane_at|store_at|at)( : kOutside)?, ", call) for call in calls), calls
-    assert kernels.count("lane_at = norm_lane(") == 1 and len(re.findall(r"= norm_turn\(|return norm_turn\(", kernels)) == 1
+    assert len(calls) == 7 and all(re.match(r"(on \? |\w*row \+ k \* rows < a\.C \? )?(lane_at|store_at|at)( : kOutside)?, (k|\(first \+ j\)) \* turn", call) for call in calls), calls
+    assert kernels.count("lane_at = norm_lane(in, row, a.T, t0),") + kernels.count("lane_at = norm_lane(in, row, a.T, t0);") == kernels.count("turn = norm_turn(rows, a.T);") == 1
+    assert kernels.count("const unsigned at = norm_store_at(lane, shared);") == 1
 
 
 HELD = {"8": (256, 8), "16": (256, 16), "few": (256, 16), "half": (512, 8), "half_16": (512, 16), "wide": (1024, 8), "wide_16": (1024, 16)}      # threads, channels of each
