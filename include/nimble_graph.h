@@ -376,8 +376,10 @@ enum {
                                    for bit. The plan passes a self-check at ng_capture or the capture fails.
                                    A graph with attention operators (or norm, dropout and position bias) has a plan if its tasks are small ones: no
                                    attention over many queries (more than 768 pairs of 16 columns and 64 keys, where
-                                   32 columns are exceeded), no kernel for large images, no gradients of convolutions
-                                   and batch-norms. Without a plan the mode is no candidate of NG_MODE_AUTO, and this mode,
+                                   32 columns are exceeded) or with a bias of distances, no layer norm whose
+                                   kernel (ng_planned_task_kernel) is a "half", "wide" or "many" one, as many channels
+                                   of many tokens get, and no gradients of one, no kernel for large images, no
+                                   gradients of convolutions and batch-norms. Without a plan the mode is no candidate of NG_MODE_AUTO, and this mode,
                                    ng_replay_static and ng_resident_dry_plan return NG_ESTATE. */
     NG_MODE_AUTO = 5          /* the default: whichever of modes 0, 1 and 4 was fastest in a short trial at ng_capture (an
                                    ahead-of-time choice like the rest of the schedule: DAGs of many tiny tasks

@@ -209,7 +209,7 @@ int plan_resident(const ng_graph* g, int n_wg, int xcds, const PlanKnobs& knobs,
 bool resident_plan_is_consistent(const ng_graph* g, const ResidentPlan& plan);
 // Graphs with attention have a device-resident plan if the attention build has all their kernels; without attention: true.
 bool has_resident_plan(const std::vector<Task>& tasks);
-constexpr const char* kNoResidentPlan = "this graph has no device-resident plan: it has attention operators next to kernels for many columns, large images or training";
+constexpr const char* kNoResidentPlan = "this graph has no device-resident plan: it has attention or block operators next to kernels that are only launched (many columns, a bias of distances, gradients of norms, wide norms, large images or training)";
 // ng_runtime.hip
 void destroy_runtime(ng_graph* g);
 }  // namespace ng

@@ -831,17 +831,18 @@ NormPlan norm_plan(const ng_graph* g, int v) {
     } else if (T < 4) {
         p.kid = one_of(KID_NORM_S16, KID_NORM_DX_S16, KID_NORM_DG_S16);
     } else {
-        // Threads side by side along the tokens: as many as leave 64 workgroups, 128 of more than 256 threads, 256 of more than 512 (few workgroups have few
-        // rows of sums to join: forward and both gradients of 4 images of 256 channels, 400 tokens with at least 64 / 128 / 256 workgroups 15.4 /
-        // 16.8 / 19.5 us, of 6 images of 520 channels, 333 tokens, where 64 are of 1024 threads, 27.0 / 21.6 / 24.9; both gradients of 16
-        // images of 1000 channels, 300 tokens in 160 of 1024 threads 29.3, in twice as many of 512 26.2), since what a workgroup reads of a channel
-        // should be whole lines of memory. TB/s of the forward kernel with 2 / 4 / 8 of them, 16 images of 512 channels, 8192 tokens 3.3 / 4.1 / 5.1, of
-        // 1024 channels, 4096 tokens 2.9 / 3.9 / 4.8; both gradients in one launch 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9. Eight take 512 threads for more than 256
-        // channels, 1024 for more than 512 (forward: 1024), or 16 channels a thread, in fewer and larger workgroups: not faster where the tensors come out of the 256 MB cache
-        // behind the L2s (4 images of 2048 channels, 4096 tokens 4: 44 us, 8: 51), so only for larger ones (both gradients of 8
-        // images of 1024 channels, 4096 tokens, 400 MB, 4: 121, 8: 115; of 2048 tokens 49 and 58). A forward kernel of 512 threads with 16 channels each takes the place of 1024 with 8: 123 -> 113 us and, in
-        // the cache, 53 -> 39 (16 and 8 images of 1024 channels, 4096 tokens, 8 side by side). Gradients of 16 channels a thread read dy twice, but twice as
-        // many tokens side by side: both of 2 images of 4096 channels, 8192 / 2000 tokens 2: 397 / 71, 4: 313 / 67 us, of 8 of 2048, 4096 tokens 4: 262, 8: 225.
+        // Threads side by side along the tokens, 1, 2, 4 or 8 with four tokens each: as many as the rules below allow, because what a workgroup
+        // reads of a channel should be whole lines of memory. (Images x channels x tokens; both: the gradients in one launch.)
+        //   TB/s with 2 / 4 / 8: forward of 16 x 512 x 8192 3.3 / 4.1 / 5.1, of 16 x 1024 x 4096 2.9 / 3.9 / 4.8; both 3.3 / 3.7 / 4.3 and 2.8 / 3.5 / 3.9.
+        // Rule 1: at least 64 workgroups, 128 of more than 256 threads, 256 of more than 512; few of them have few rows of sums to join.
+        //   us with 64 / 128 / 256 at least: forward and both of 4 x 256 x 400 15.4 / 16.8 / 19.5, of 6 x 520 x 333, where 64 are of 1024 threads,
+        //   27.0 / 21.6 / 24.9. Both of 16 x 1000 x 300 in 160 workgroups of 1024 threads 29.3, in twice as many of 512 26.2.
+        // Rule 2: eight with more than 256 threads only for tensors beyond the 256 MB cache behind the L2s.
+        //   us with 4 / 8: forward of 4 x 2048 x 4096 (in the cache) 44 / 51, both of 8 x 1024 x 2048 (in it) 49 / 58, of 8 x 1024 x 4096 121 / 115.
+        // Rule 3: more channels than 512 threads of 8 hold: forward in 512 threads of 16 channels each, not 1024 of 8.
+        //   us with 1024 / 512: 16 x 1024 x 4096 123 / 113, 8 x 1024 x 4096 (in the cache) 53 / 39, eight side by side.
+        // Rule 4: more than 1024 threads of 8 hold: 16 each. The gradients then read dy twice, with twice as many tokens side by side.
+        //   us of both with 8 / 16 channels a thread: 2 x 4096 x 8192 397 / 313, 2 x 4096 x 2000 71 / 67, 8 x 2048 x 4096 262 / 225.
         const bool large = (double)x.elems() * 4 * (which == 0 ? 2 : 3) > 268435456.0;
         long threads = 0;
         for (int log2 = 3; log2 >= 0; --log2) {
