@@ -42,8 +42,8 @@ enum {
     NG_EINVAL = -1, /* bad argument (null pointer, unknown id, unknown op, bad parameter) */
     NG_ESHAPE = -2, /* operand shapes do not fit the operator */
     NG_ESTATE = -3, /* call made in the wrong phase */
-    NG_ENOMEM = -4, /* arena too small or too few streams */
-    NG_EHIP = -5    /* a HIP runtime call failed; text in ng_last_error() */
+    NG_ENOMEM = -4, /* arena too small, too few streams, or no host memory left */
+    NG_EHIP = -5    /* a HIP runtime call failed or something threw; text in ng_last_error() */
 };
 
 /* Operator vocabulary: one node = one GPU task (the paper's operators may be several

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <new>
 
 #include "ng_internal.h"
@@ -345,6 +346,25 @@ const char* infer_shape(const ng_graph* g, int op, ng_op_params& p, const int* p
 
 }  // namespace
 
+namespace ng {
+int thrown(const ng_graph* g) noexcept {
+    ng_graph* to = const_cast<ng_graph*>(g);
+    try {
+        try {
+            throw;
+        } catch (const std::bad_alloc&) {
+            return to->fail(NG_ENOMEM, "out of host memory");
+        } catch (const std::exception& e) {
+            return to->fail(NG_EHIP, "exception: %s", e.what());
+        } catch (...) {
+            return to->fail(NG_EHIP, "exception of an unknown type");
+        }
+    } catch (...) {                                             // no memory for the message either: the one before it stays
+        return NG_ENOMEM;
+    }
+}
+}  // namespace ng
+
 extern "C" {
 
 const char* ng_version(void) { return "nimble_graph 0.1 (gfx950)"; }
@@ -363,7 +383,7 @@ void ng_destroy(ng_graph* g) {
 
 const char* ng_last_error(const ng_graph* g) { return g ? g->err.c_str() : "null graph"; }
 
-int ng_add_input(ng_graph* g, const int64_t nchw[4], int* id) {
+int ng_add_input(ng_graph* g, const int64_t nchw[4], int* id) try {
     if (!g) return NG_EINVAL;
     if (!nchw || !id) return g->fail(NG_EINVAL, "ng_add_input: null argument");
     if (g->phase != BUILDING) return g->fail(NG_ESTATE, "ng_add_input: registration is closed");
@@ -375,10 +395,10 @@ int ng_add_input(ng_graph* g, const int64_t nchw[4], int* id) {
     g->nodes.push_back(nd);
     *id = (int)g->nodes.size() - 1;
     return NG_OK;
-}
+} NG_THROWN(g)
 
 int ng_add_node(ng_graph* g, int op_kind, const ng_op_params* p, const int* preds, int n_preds,
-                const void* const* dev_weights, int n_weights, int* id) {
+                const void* const* dev_weights, int n_weights, int* id) try {
     if (!g) return NG_EINVAL;
     if (!id || n_preds < 0 || n_weights < 0 || (n_preds > 0 && !preds) || (n_weights > 0 && !dev_weights))
         return g->fail(NG_EINVAL, "ng_add_node: null or negative argument");
@@ -401,34 +421,34 @@ int ng_add_node(ng_graph* g, int op_kind, const ng_op_params* p, const int* pred
     g->nodes.push_back(std::move(nd));
     *id = (int)g->nodes.size() - 1;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_mark_output(ng_graph* g, int id) {
+int ng_mark_output(ng_graph* g, int id) try {
     if (!g) return NG_EINVAL;
     if (id < 0 || id >= (int)g->nodes.size()) return g->fail(NG_EINVAL, "ng_mark_output: no node %d", id);
     g->nodes[id].is_output = true;
     return NG_OK;
-}
+} NG_THROWN(g)
 
 int ng_num_nodes(const ng_graph* g) { return g ? (int)g->nodes.size() : NG_EINVAL; }
 
-int ng_node_shape(const ng_graph* g, int id, int64_t nchw[4]) {
+int ng_node_shape(const ng_graph* g, int id, int64_t nchw[4]) try {
     if (!g || !nchw || id < 0 || id >= (int)g->nodes.size()) return NG_EINVAL;
     const Shape& s = g->nodes[id].out;
     nchw[0] = s.n, nchw[1] = s.c, nchw[2] = s.h, nchw[3] = s.w;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_set_assignment(ng_graph* g, int assignment) {
+int ng_set_assignment(ng_graph* g, int assignment) try {
     if (!g) return NG_EINVAL;
     if (g->phase != BUILDING) return g->fail(NG_ESTATE, "ng_set_assignment: already scheduled");
     if (assignment != NG_ASSIGN_ALGORITHM1 && assignment != NG_ASSIGN_EXACT)
         return g->fail(NG_EINVAL, "ng_set_assignment: unknown assignment %d", assignment);
     g->assignment = assignment;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_schedule(ng_graph* g) {
+int ng_schedule(ng_graph* g) try {
     if (!g) return NG_EINVAL;
     if (g->phase != BUILDING) return g->fail(NG_ESTATE, "ng_schedule: already scheduled");
     if (g->nodes.empty()) return g->fail(NG_EINVAL, "ng_schedule: empty graph");
@@ -440,10 +460,10 @@ int ng_schedule(ng_graph* g) {
     for (const Node& nd : g->nodes) g->trainable = g->trainable || nd.op == NG_OP_SGD_UPDATE;
     g->phase = SCHEDULED;
     return NG_OK;
-}
+} NG_THROWN(g)
 
 int ng_schedule_sizes(const ng_graph* g, int* n_nodes, int* n_streams, int* n_chains, int* n_meg_edges,
-                      int* n_matching, int* n_sync, int* n_events) {
+                      int* n_matching, int* n_sync, int* n_events) try {
     if (!g) return NG_EINVAL;
     if (g->phase < SCHEDULED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_schedule_sizes: call ng_schedule first");
     const Schedule& s = g->sched;
@@ -455,10 +475,10 @@ int ng_schedule_sizes(const ng_graph* g, int* n_nodes, int* n_streams, int* n_ch
     if (n_sync) *n_sync = (int)s.sync.size();
     if (n_events) *n_events = s.n_events;
     return NG_OK;
-}
+} NG_THROWN(g)
 
 int ng_get_schedule(const ng_graph* g, int* order, int* stream_of, int* chain_of, int* event_of,
-                    int* meg_src, int* meg_dst, int* sync_src, int* sync_dst) {
+                    int* meg_src, int* meg_dst, int* sync_src, int* sync_dst) try {
     if (!g) return NG_EINVAL;
     if (g->phase < SCHEDULED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_get_schedule: call ng_schedule first");
     const Schedule& s = g->sched;
@@ -477,9 +497,9 @@ int ng_get_schedule(const ng_graph* g, int* order, int* stream_of, int* chain_of
         if (sync_dst) sync_dst[i] = s.sync[i].second;
     }
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_get_scaffold(const ng_graph* g, int* fork, int* n_fork, int* join, int* n_join) {
+int ng_get_scaffold(const ng_graph* g, int* fork, int* n_fork, int* join, int* n_join) try {
     if (!g) return NG_EINVAL;
     if (g->phase < SCHEDULED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_get_scaffold: call ng_schedule first");
     const Schedule& s = g->sched;
@@ -488,9 +508,9 @@ int ng_get_scaffold(const ng_graph* g, int* fork, int* n_fork, int* join, int* n
     if (n_fork) *n_fork = (int)s.fork.size();
     if (n_join) *n_join = (int)s.join.size();
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_plan_memory(ng_graph* g, size_t* arena_bytes) {
+int ng_plan_memory(ng_graph* g, size_t* arena_bytes) try {
     if (!g) return NG_EINVAL;
     if (g->phase < SCHEDULED) return g->fail(NG_ESTATE, "ng_plan_memory: call ng_schedule first");
     if (g->phase > PLANNED) return g->fail(NG_ESTATE, "ng_plan_memory: already bound");
@@ -573,38 +593,38 @@ int ng_plan_memory(ng_graph* g, size_t* arena_bytes) {
     g->phase = PLANNED;
     if (arena_bytes) *arena_bytes = top;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_set_memory_reuse(ng_graph* g, int on) {
+int ng_set_memory_reuse(ng_graph* g, int on) try {
     if (!g) return NG_EINVAL;
     if (g->phase > SCHEDULED) return g->fail(NG_ESTATE, "ng_set_memory_reuse: the memory plan is already made");
     g->memory_reuse = on != 0;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_set_launch_fusion(ng_graph* g, int on) {
+int ng_set_launch_fusion(ng_graph* g, int on) try {
     if (!g) return NG_EINVAL;
     if (g->phase >= BOUND) return g->fail(NG_ESTATE, "ng_set_launch_fusion: the task table is already built");
     g->launch_fusion = on != 0;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_set_unsplit_products(ng_graph* g, int on) {
+int ng_set_unsplit_products(ng_graph* g, int on) try {
     if (!g) return NG_EINVAL;
     if (g->phase >= BOUND) return g->fail(NG_ESTATE, "ng_set_unsplit_products: the task table is already built");
     g->unsplit_products = on != 0;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_get_offsets(const ng_graph* g, size_t* offset, size_t* bytes) {
+int ng_get_offsets(const ng_graph* g, size_t* offset, size_t* bytes) try {
     if (!g) return NG_EINVAL;
     if (g->phase < PLANNED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_get_offsets: call ng_plan_memory first");
     if (offset) std::copy(g->offset.begin(), g->offset.end(), offset);
     if (bytes) std::copy(g->bytes.begin(), g->bytes.end(), bytes);
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_critical_path(const ng_graph* g, const float* t, float* total, int* path, int* n_path) {
+int ng_critical_path(const ng_graph* g, const float* t, float* total, int* path, int* n_path) try {
     if (!g || !t) return NG_EINVAL;
     const int n = (int)g->nodes.size();
     if (n == 0) return NG_EINVAL;
@@ -627,9 +647,9 @@ int ng_critical_path(const ng_graph* g, const float* t, float* total, int* path,
     if (n_path) *n_path = (int)rev.size();
     if (path) std::reverse_copy(rev.begin(), rev.end(), path);
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_task_work(const ng_graph* g, int id, double* bytes, double* flops) {
+int ng_task_work(const ng_graph* g, int id, double* bytes, double* flops) try {
     if (!g || id < 0 || id >= (int)g->nodes.size()) return NG_EINVAL;
     const Node& nd = g->nodes[id];
     const double out = (double)nd.out.elems();
@@ -695,6 +715,6 @@ int ng_task_work(const ng_graph* g, int id, double* bytes, double* flops) {
     if (bytes) *bytes = b;
     if (flops) *flops = f;
     return NG_OK;
-}
+} NG_THROWN(g)
 
 }  // extern "C"

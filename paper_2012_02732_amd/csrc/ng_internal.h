@@ -173,6 +173,11 @@ struct ng_graph {
 };
 
 namespace ng {
+// Nothing throws across the C boundary: an entry's body is a function try block (`int ng_x(..) try { .. } NG_THROWN(g)`), in which what the
+// standard library throws, or a runtime below, becomes a message and a code.
+int thrown(const ng_graph* g) noexcept;
+#define NG_THROWN(g) catch (...) { return ng::thrown(g); }
+#define NG_THROWN_NULL(g) catch (...) { return (void)ng::thrown(g), nullptr; }
 // ng_schedule.cpp
 void compute_schedule(int n, const std::vector<std::pair<int, int>>& edges, Schedule& out, bool exact);
 // ng_tasks.hip: fill the launch descriptor of node v (addresses resolved against `arena`;

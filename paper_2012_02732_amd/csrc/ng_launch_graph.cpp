@@ -372,7 +372,7 @@ struct TaskView {
 };
 }  // namespace
 
-extern "C" int ng_get_graph_edges(ng_graph* g, int fuse, int* launched_by, int* n_edges, int* src, int* dst, int max_edges) {
+extern "C" int ng_get_graph_edges(ng_graph* g, int fuse, int* launched_by, int* n_edges, int* src, int* dst, int max_edges) try {
     if (!g) return NG_EINVAL;
     if (g->phase < PLANNED) return g->fail(NG_ESTATE, "ng_get_graph_edges: call ng_plan_memory first");
     if (max_edges < 0 || (max_edges > 0 && (!src || !dst))) return g->fail(NG_EINVAL, "ng_get_graph_edges: bad edge arrays");
@@ -403,9 +403,9 @@ extern "C" int ng_get_graph_edges(ng_graph* g, int fuse, int* launched_by, int* 
     if (n_edges) *n_edges = count;
     if (count > max_edges && max_edges > 0) return g->fail(NG_ENOMEM, "ng_get_graph_edges: %d edges, room for %d", count, max_edges);
     return NG_OK;
-}
+} NG_THROWN(g)
 
-extern "C" int ng_get_single_launches(ng_graph* g, int* position, int* n_launches) {
+extern "C" int ng_get_single_launches(ng_graph* g, int* position, int* n_launches) try {
     if (!g) return NG_EINVAL;
     if (g->phase < PLANNED) return g->fail(NG_ESTATE, "ng_get_single_launches: call ng_plan_memory first");
     TaskView view(g);
@@ -424,9 +424,9 @@ extern "C" int ng_get_single_launches(ng_graph* g, int* position, int* n_launche
     }
     if (n_launches) *n_launches = (int)launches.size();
     return NG_OK;
-}
+} NG_THROWN(g)
 
-extern "C" const char* ng_planned_task_kernel(ng_graph* g, int id) {
+extern "C" const char* ng_planned_task_kernel(ng_graph* g, int id) try {
     if (!g) return nullptr;
     if (g->phase < PLANNED) return g->fail(NG_ESTATE, "ng_planned_task_kernel: call ng_plan_memory first"), nullptr;
     if (id < 0 || id >= (int)g->nodes.size()) return g->fail(NG_EINVAL, "ng_planned_task_kernel: no node %d", id), nullptr;
@@ -434,4 +434,4 @@ extern "C" const char* ng_planned_task_kernel(ng_graph* g, int id) {
     if (view.rc != NG_OK) return nullptr;
     const char* name = g->tasks[id].name;
     return name ? name : "";
-}
+} NG_THROWN_NULL(g)

@@ -887,12 +887,12 @@ bool resident_plan_is_consistent(const ng_graph* g, const ResidentPlan& plan) {
 }  // namespace ng
 
 extern "C" int ng_resident_dry_plan(ng_graph* g, int n_workgroups, int xcds, double* expected_us, int* n_entries,
-                                    int* n_far_edges, int* coverage_ok) {
+                                    int* n_far_edges, int* coverage_ok) try {
     return ng_resident_dry_plan_setting(g, 0, n_workgroups, xcds, expected_us, n_entries, n_far_edges, coverage_ok);
-}
+} NG_THROWN(g)
 
 extern "C" int ng_resident_dry_plan_setting(ng_graph* g, int setting, int n_workgroups, int xcds, double* expected_us,
-                                            int* n_entries, int* n_far_edges, int* coverage_ok) {
+                                            int* n_entries, int* n_far_edges, int* coverage_ok) try {
     using namespace ng;
     if (!g) return NG_EINVAL;
     if (g->phase < PLANNED) return g->fail(NG_ESTATE, "ng_resident_dry_plan: call ng_plan_memory first");
@@ -923,4 +923,4 @@ extern "C" int ng_resident_dry_plan_setting(ng_graph* g, int setting, int n_work
     g->dry_run = false;
     g->tasks.swap(saved);
     return rc;
-}
+} NG_THROWN(g)

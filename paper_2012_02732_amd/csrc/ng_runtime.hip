@@ -643,7 +643,7 @@ using namespace ng;
 
 extern "C" {
 
-int ng_bind(ng_graph* g, void* arena, size_t arena_bytes, void* const* hip_streams, int n_streams) {
+int ng_bind(ng_graph* g, void* arena, size_t arena_bytes, void* const* hip_streams, int n_streams) try {
     if (!g) return NG_EINVAL;
     if (g->phase < PLANNED) return g->fail(NG_ESTATE, "ng_bind: call ng_plan_memory first");
     if (!arena || !hip_streams) return g->fail(NG_EINVAL, "ng_bind: null arena or stream array");
@@ -662,6 +662,7 @@ int ng_bind(ng_graph* g, void* arena, size_t arena_bytes, void* const* hip_strea
         return g->fail(NG_EINVAL, "ng_bind: arena is not device memory");
     }
     destroy_runtime(g);
+    g->phase = PLANNED;                                        // until all of it is there: what fails on the way leaves nothing that could be replayed
     g->rt = new Runtime();
     Runtime& rt = *g->rt;
     rt.arena = static_cast<char*>(arena);
@@ -764,9 +765,9 @@ int ng_bind(ng_graph* g, void* arena, size_t arena_bytes, void* const* hip_strea
     NG_HIP(hipEventCreate(&rt.t_stop));
     g->phase = BOUND;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_capture(ng_graph* g) {
+int ng_capture(ng_graph* g) try {
     if (!g) return NG_EINVAL;
     if (g->phase < BOUND) return g->fail(NG_ESTATE, "ng_capture: call ng_bind first");
     Runtime& rt = *g->rt;
@@ -827,26 +828,26 @@ int ng_capture(ng_graph* g) {
         rt.trained.clear();
     }
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_auto_mode(const ng_graph* g, int* mode, float* trial_us) {
+int ng_auto_mode(const ng_graph* g, int* mode, float* trial_us) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_auto_mode: call ng_capture first");
     if (mode) *mode = g->auto_mode;
     if (trial_us)
         for (int i = 0; i < 3; ++i) trial_us[i] = g->auto_trial_us[i];
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_graph_multi_check(const ng_graph* g, int* state, int* replays_compared) {
+int ng_graph_multi_check(const ng_graph* g, int* state, int* replays_compared) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_graph_multi_check: call ng_capture first");
     if (state) *state = g->graph_multi_state;
     if (replays_compared) *replays_compared = g->graph_multi_checked;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_graph_multi_recheck(ng_graph* g, int replays) {
+int ng_graph_multi_recheck(ng_graph* g, int replays) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_graph_multi_recheck: call ng_capture first");
     if (replays < 1 || replays > 100000) return g->fail(NG_EINVAL, "ng_graph_multi_recheck: replays must be 1..100000");
@@ -866,27 +867,27 @@ int ng_graph_multi_recheck(ng_graph* g, int replays) {
     if (rc != NG_OK) return rc;
     pick_auto_mode(g);
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_graph_multi_distrust(ng_graph* g) {
+int ng_graph_multi_distrust(ng_graph* g) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_graph_multi_distrust: call ng_capture first");
     g->graph_multi_state = -1;
     pick_auto_mode(g);
     return NG_OK;
-}
+} NG_THROWN(g)
 
 void* ng_tensor_ptr(const ng_graph* g, int id) {
     if (!g || g->phase < BOUND || id < 0 || id >= (int)g->nodes.size()) return nullptr;
     return g->rt->arena + g->offset[id];
 }
 
-int ng_replay_mode(ng_graph* g, int mode) {
+int ng_replay_mode(ng_graph* g, int mode) try {
     if (!g) return NG_EINVAL;
     if (mode < NG_MODE_GRAPH_MULTI || mode > NG_MODE_AUTO) return g->fail(NG_EINVAL, "ng_replay_mode: unknown mode %d", mode);
     g->mode = mode;
     return NG_OK;
-}
+} NG_THROWN(g)
 
 static int enqueue_replay(ng_graph* g) {
     Runtime& rt = *g->rt;
@@ -909,14 +910,14 @@ static int enqueue_replay(ng_graph* g) {
     }
 }
 
-int ng_replay(ng_graph* g) {
+int ng_replay(ng_graph* g) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_replay: call ng_capture first");
     if (int rc = arrivals_ready(g)) return rc;
     if (int rc = enqueue_replay(g)) return rc;
     replay_enqueued(*g->rt);
     return NG_OK;
-}
+} NG_THROWN(g)
 
 // ---- device-resident replay that allocates nothing -------------------------------------------
 // For callers that cannot allocate (code under HIP graph capture, tight serving loops, harnesses that
@@ -937,7 +938,7 @@ __global__ __launch_bounds__(256) void zero_words_kernel(unsigned* p, size_t wor
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) p[i] = 0u;
 }
 
-int ng_replay_static(ng_graph* g) {
+int ng_replay_static(ng_graph* g) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_replay_static: call ng_capture first");
     Runtime& rt = *g->rt;
@@ -976,9 +977,9 @@ int ng_replay_static(ng_graph* g) {
     NG_HIP(hipLaunchKernel(resident_kernel_handle(rt.resident_build), dim3(rt.n_wg), dim3(kGroup), args, 0, origin));
     replay_enqueued(rt);
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_sync(ng_graph* g) {
+int ng_sync(ng_graph* g) try {
     if (!g) return NG_EINVAL;
     if (g->phase < BOUND) return g->fail(NG_ESTATE, "ng_sync: call ng_bind first");
     NG_HIP(hipStreamSynchronize(g->rt->streams[0]));
@@ -993,9 +994,9 @@ int ng_sync(ng_graph* g) {
         return g->fail(NG_EHIP, "device-resident replay: the wait before task %d ran out of spins; outputs are incomplete", task);
     }
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_resident_config(ng_graph* g, int workgroups_per_cu, int xcds, unsigned spin_limit, int device_scope_everywhere) {
+int ng_resident_config(ng_graph* g, int workgroups_per_cu, int xcds, unsigned spin_limit, int device_scope_everywhere) try {
     if (!g) return NG_EINVAL;
     if (workgroups_per_cu < 0 || workgroups_per_cu > 8) return g->fail(NG_EINVAL, "ng_resident_config: workgroups_per_cu must be 0..8");
     if (xcds < 0 || xcds > 8) return g->fail(NG_EINVAL, "ng_resident_config: xcds must be 0..8");
@@ -1007,24 +1008,24 @@ int ng_resident_config(ng_graph* g, int workgroups_per_cu, int xcds, unsigned sp
     }
     g->resident_spin_limit = spin_limit ? spin_limit : kDefaultSpinLimit;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_resident_plan_trials(ng_graph* g, int trials) {
+int ng_resident_plan_trials(ng_graph* g, int trials) try {
     if (!g) return NG_EINVAL;
     if (trials < 1 || trials > 8) return g->fail(NG_EINVAL, "ng_resident_plan_trials: trials must be 1..8");
     if (g->phase >= CAPTURED) return g->fail(NG_ESTATE, "ng_resident_plan_trials: the plan is fixed at ng_capture");
     g->resident_plan_trials = trials;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_resident_plan_kept(const ng_graph* g, int* setting) {
+int ng_resident_plan_kept(const ng_graph* g, int* setting) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_resident_plan_kept: call ng_capture first");
     if (setting) *setting = g->resident_plan_kept;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_resident_trace(ng_graph* g, int enable, unsigned long long* ticks) {
+int ng_resident_trace(ng_graph* g, int enable, unsigned long long* ticks) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_resident_trace: call ng_capture first");
     if (!g->rt->d_records) return g->fail(NG_ESTATE, "ng_resident_trace: %s", kNoResidentPlan);
@@ -1069,24 +1070,24 @@ int ng_resident_trace(ng_graph* g, int enable, unsigned long long* ticks) {
         rt.plan.trace = nullptr;
     }
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_resident_xcd_mapping(const ng_graph* g, int* verified) {
+int ng_resident_xcd_mapping(const ng_graph* g, int* verified) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_resident_xcd_mapping: call ng_capture first");
     if (verified) *verified = g->rt->xcd_mapping_ok ? 1 : 0;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_resident_fusion(const ng_graph* g, int* host_of) {
+int ng_resident_fusion(const ng_graph* g, int* host_of) try {
     if (!g || !host_of) return NG_EINVAL;
     if (g->phase < CAPTURED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_resident_fusion: call ng_capture first");
     for (size_t v = 0; v < g->nodes.size(); ++v)
         host_of[v] = v >= g->rt->fused_into.size() ? -1 : (g->rt->elided[v] ? -2 : g->rt->fused_into[v]);
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_resident_sizes(const ng_graph* g, int* n_workgroups, int* n_entries, int* xcds, double* expected_us) {
+int ng_resident_sizes(const ng_graph* g, int* n_workgroups, int* n_entries, int* xcds, double* expected_us) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return const_cast<ng_graph*>(g)->fail(NG_ESTATE, "ng_resident_sizes: call ng_capture first");
     if (n_workgroups) *n_workgroups = g->rt->n_wg;
@@ -1094,7 +1095,7 @@ int ng_resident_sizes(const ng_graph* g, int* n_workgroups, int* n_entries, int*
     if (xcds) *xcds = g->rt->xcds;
     if (expected_us) *expected_us = g->rt->est_us;
     return NG_OK;
-}
+} NG_THROWN(g)
 
 // Time per node of a graph that is a chain of `reps` copies of one kernel node, launched on
 // the origin stream: the device runs the copies back to back, each waiting for the one before.
@@ -1144,7 +1145,7 @@ static int chain_time(ng_graph* g, const void* fn, const unsigned grid[3], const
     return rc;
 }
 
-int ng_time_replay(ng_graph* g, int reps, float* avg_us) {
+int ng_time_replay(ng_graph* g, int reps, float* avg_us) try {
     if (!g) return NG_EINVAL;
     if (g->phase < CAPTURED) return g->fail(NG_ESTATE, "ng_time_replay: call ng_capture first");
     if (reps <= 0 || !avg_us) return g->fail(NG_EINVAL, "ng_time_replay: bad argument");
@@ -1159,9 +1160,9 @@ int ng_time_replay(ng_graph* g, int reps, float* avg_us) {
     NG_HIP(hipEventElapsedTime(&ms, rt.t_start, rt.t_stop));
     *avg_us = ms * 1000.f / (float)reps;
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_time_chain(ng_graph* g, int id, int reps, float* us_per_node) {
+int ng_time_chain(ng_graph* g, int id, int reps, float* us_per_node) try {
     if (!g) return NG_EINVAL;
     if (g->phase < BOUND) return g->fail(NG_ESTATE, "ng_time_chain: call ng_bind first");
     if (id < -1 || id >= (int)g->nodes.size() || reps <= 0 || reps > 10000 || !us_per_node)
@@ -1174,9 +1175,9 @@ int ng_time_chain(ng_graph* g, int id, int reps, float* us_per_node) {
     Task& t = g->tasks[id];
     if (!t.fn) return NG_OK;
     return chain_time(g, t.fn, t.grid, t.block, t.lds_bytes, t.args, reps, us_per_node);
-}
+} NG_THROWN(g)
 
-int ng_time_task(ng_graph* g, int id, int reps, float* isolated_us) {
+int ng_time_task(ng_graph* g, int id, int reps, float* isolated_us) try {
     if (!g) return NG_EINVAL;
     if (g->phase < BOUND) return g->fail(NG_ESTATE, "ng_time_task: call ng_bind first");
     if (id < 0 || id >= (int)g->nodes.size() || reps <= 0 || !isolated_us) return g->fail(NG_EINVAL, "ng_time_task: bad argument");
@@ -1189,7 +1190,7 @@ int ng_time_task(ng_graph* g, int id, int reps, float* isolated_us) {
     if (int rc = ng_time_chain(g, id, reps, &c)) return rc;
     *isolated_us = std::max(c - rt.empty_chain_us, 0.f);
     return NG_OK;
-}
+} NG_THROWN(g)
 
 // A kernel that is launched by itself, to be timed or traced.
 struct SoloLaunch {
@@ -1239,7 +1240,7 @@ static bool executed_launch(const ng_graph* g, int id, int mode, SoloLaunch& out
     return true;
 }
 
-int ng_time_task_device(ng_graph* g, int id, int as_executed, int reps, float* median_us, float* min_us) {
+int ng_time_task_device(ng_graph* g, int id, int as_executed, int reps, float* median_us, float* min_us) try {
     if (!g) return NG_EINVAL;
     if (g->phase < (as_executed ? CAPTURED : BOUND)) return g->fail(NG_ESTATE, "ng_time_task_device: call %s first", as_executed ? "ng_capture" : "ng_bind");
     if (id < 0 || id >= (int)g->nodes.size() || reps <= 0 || reps > 100000 || !median_us) return g->fail(NG_EINVAL, "ng_time_task_device: bad argument");
@@ -1277,9 +1278,9 @@ int ng_time_task_device(ng_graph* g, int id, int as_executed, int reps, float* m
     *median_us = us[us.size() / 2];
     if (min_us) *min_us = us.front();
     return NG_OK;
-}
+} NG_THROWN(g)
 
-int ng_launch_task_solo(ng_graph* g, int id, int as_executed) {
+int ng_launch_task_solo(ng_graph* g, int id, int as_executed) try {
     if (!g) return NG_EINVAL;
     if (g->phase < (as_executed ? CAPTURED : BOUND)) return g->fail(NG_ESTATE, "ng_launch_task_solo: call %s first", as_executed ? "ng_capture" : "ng_bind");
     if (id < -1 || id >= (int)g->nodes.size()) return g->fail(NG_EINVAL, "ng_launch_task_solo: no node %d", id);
@@ -1296,15 +1297,15 @@ int ng_launch_task_solo(ng_graph* g, int id, int as_executed) {
     }
     NG_HIP(hipStreamSynchronize(s));
     return NG_OK;
-}
+} NG_THROWN(g)
 
-const char* ng_task_kernel_executed(const ng_graph* g, int id) {
+const char* ng_task_kernel_executed(const ng_graph* g, int id) try {
     if (!g || g->phase < CAPTURED || id < 0 || id >= (int)g->tasks.size()) return "";
     SoloLaunch l;
     return executed_launch(g, id, g->mode, l) ? l.name : "";
-}
+} NG_THROWN_NULL(g)
 
-int ng_time_launch_floor(ng_graph* g, int reps, float* median_us) {
+int ng_time_launch_floor(ng_graph* g, int reps, float* median_us) try {
     if (!g) return NG_EINVAL;
     if (g->phase < BOUND) return g->fail(NG_ESTATE, "ng_time_launch_floor: call ng_bind first");
     if (reps <= 0 || reps > 100000 || !median_us) return g->fail(NG_EINVAL, "ng_time_launch_floor: bad argument");
@@ -1320,11 +1321,11 @@ int ng_time_launch_floor(ng_graph* g, int reps, float* median_us) {
     std::sort(us.begin(), us.end());
     *median_us = us[us.size() / 2];
     return NG_OK;
-}
+} NG_THROWN(g)
 
-const char* ng_task_kernel(const ng_graph* g, int id) {
+const char* ng_task_kernel(const ng_graph* g, int id) try {
     if (!g || g->phase < BOUND || id < 0 || id >= (int)g->tasks.size()) return "";
     return g->tasks[id].name;
-}
+} NG_THROWN_NULL(g)
 
 }  // extern "C"
